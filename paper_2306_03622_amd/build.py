@@ -2,7 +2,7 @@
 
     python -m paper_2306_03622_amd.build [--jobs N] [--sanitize]
 
-``libtorpor.so`` holds the C ABI of include/torpor.h and include/torpor_plan.h with all
+``libtorpor.so`` holds the C ABI of include/torpor.h, include/torpor_plan.h and include/torpor_ops.h with all
 kernels; ``libtorpor_probe.so`` the peak probes of include/torpor_probe.h that the
 benchmark measures its rooflines against. ``libtorpor_host.so`` is the same host-side bookkeeping (validation, chunk
 plan, arena) compiled with g++ alone, optionally with ASan/UBSan, for host-only tests.
@@ -24,10 +24,11 @@ HOST_LIB = os.path.join(PKG, "libtorpor_host.so")
 PROBE_LIB = os.path.join(PKG, "libtorpor_probe.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-CORE = ["core/model.cpp", "core/arena.cpp", "core/partition.cpp", "core/sched.cpp", "core/plan_api.cpp", "core/errors.cpp"]
-HIP_HOST = ["hip/runtime.cpp", "hip/executors.cpp", "hip/trace.cpp"]
+CORE = ["core/model.cpp", "core/arena.cpp", "core/partition.cpp", "core/sched.cpp", "core/plan_api.cpp", "core/errors.cpp", "core/w4.cpp"]
+HIP_HOST = ["hip/runtime.cpp", "hip/executors.cpp", "hip/trace.cpp", "hip/ops_api.cpp"]
 PROBE = ["probe/peaks.hip"]
 KERNELS = ["hip/scratch.hip", "kernels/gemm_bf16.hip", "kernels/gemv_bf16.hip", "kernels/stem.hip", "kernels/linear_f32.hip", "kernels/norm.hip", "kernels/attention.hip",
+           "kernels/w4.hip", "kernels/attn_masked.hip",
            "kernels/pool_copy.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-Wall", f"-I{os.path.join(ROOT, 'include')}"]

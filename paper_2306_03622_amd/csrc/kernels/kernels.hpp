@@ -99,6 +99,38 @@ hipError_t embed_ln(const int32_t* ids, int M, int S, int D, int vocab, const ui
 // heads contiguous inside each) -> out bf16 [B*S][H*64]. S % 32 == 0, S <= 256.
 hipError_t attention(const uint16_t* qkv, int B, int S, int H, uint16_t* out, hipStream_t s);
 
+// A linear layer with 4-bit weights in blocked order (torpor_ops.h): y = act(x W^T + bias + res). K a multiple of the
+// group (32, 64 or 128); x from 16-byte boundaries with ldx % 8 == 0, codes and scales from 16-byte boundaries.
+struct LinearW4 {
+  const uint16_t* x = nullptr;
+  int64_t ldx = 0;
+  const uint8_t* wq = nullptr;
+  const uint16_t* scales = nullptr;
+  const uint16_t* bias = nullptr;   // bf16 [N], may be null
+  const uint16_t* res = nullptr;    // bf16, may be null
+  int64_t ldr = 0;
+  void* y = nullptr;
+  int64_t ldy = 0;
+  int y_f32 = 0;
+  int M = 0, N = 0, K = 0, group = 0;
+  int act = 0;                      // ACT_*
+};
+hipError_t linear_w4(const LinearW4& a, const Split& sp, hipStream_t s);
+
+// Attention with lengths, a window and sinks (torpor_ops.h, whose argument block it mirrors). zero_tail: rows behind a
+// sequence's last query are set to zero instead of left.
+struct Attention {
+  const uint16_t *q = nullptr, *k = nullptr, *v = nullptr;
+  uint16_t* out = nullptr;
+  int64_t qs[3] = {}, ks[3] = {}, vs[3] = {}, os[3] = {};
+  const int32_t *q_lens = nullptr, *kv_lens = nullptr;
+  int batch = 0, heads = 0, kv_heads = 0, dim = 0, q_len = 0, kv_len = 0;
+  int causal = 0, left = -1, right = -1, sinks = 0;
+  float scale = 0.f;
+  int zero_tail = 0;
+};
+hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s);
+
 // dst = src, n bf16 values (n % 8 == 0): dst 16-byte aligned, src at any element.
 hipError_t copy_aligned(const uint16_t* src, uint64_t n, uint16_t* dst, hipStream_t s);
 

@@ -114,6 +114,22 @@ class tp_sched_stats(C.Structure):
         return {k: getattr(self, k) for k, _ in self._fields_}
 
 
+class tpo_linear_w4_args(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("ldx", C.c_int64), ("wq", C.c_void_p), ("scales", C.c_void_p), ("bias", C.c_void_p),
+                ("res", C.c_void_p), ("ldr", C.c_int64), ("y", C.c_void_p), ("ldy", C.c_int64), ("y_dtype", C.c_int32),
+                ("M", C.c_int32), ("N", C.c_int32), ("K", C.c_int32), ("group", C.c_int32), ("act", C.c_int32),
+                ("work", C.c_void_p), ("work_bytes", C.c_uint64)]
+
+
+class tpo_attention_args(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_int64 * 3),
+                ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3), ("out_stride", C.c_int64 * 3),
+                ("q_lens", C.c_void_p), ("kv_lens", C.c_void_p), ("batch", C.c_int32), ("heads", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("q_len", C.c_int32), ("kv_len", C.c_int32),
+                ("causal", C.c_int32), ("window_left", C.c_int32), ("window_right", C.c_int32), ("sinks", C.c_int32),
+                ("scale", C.c_float), ("work", C.c_void_p), ("work_bytes", C.c_uint64)]
+
+
 class TorporError(RuntimeError):
     def __init__(self, status: int, msg: str):
         super().__init__(f"status {status}: {msg}")
@@ -173,8 +189,13 @@ _SIGS = {
     "tph_arena_steps": [_P, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_uint64),
                         C.POINTER(C.c_uint64), C.c_uint32, C.POINTER(C.c_uint32)],
     "tph_arena_stats": [_P, C.POINTER(tp_arena_stats_t)],
+    "tpo_w4_bytes": [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_uint64), C.POINTER(C.c_uint64)],
+    "tpo_w4_pack": [_P, _P, C.c_int32, C.c_int32, C.c_int32, _P, _P],
+    "tpo_w4_quantize": [_P, C.c_int32, C.c_int32, C.c_int32, _P, _P],
+    "tpo_linear_w4": [C.POINTER(tpo_linear_w4_args), _P],
+    "tpo_attention": [C.POINTER(tpo_attention_args), _P],
 }
-HOST_ONLY = [n for n in _SIGS if n.startswith("tph_")]
+HOST_ONLY = [n for n in _SIGS if n.startswith(("tph_", "tpo_w4_"))]
 
 _lib = None
 _host = None
@@ -494,6 +515,170 @@ def tph_alpha_update(alpha, last_ratio, new_ratio, scalar=2.0, threshold=0.04, L
     out = C.c_double()
     _check(L, L.tph_alpha_update(alpha, last_ratio, new_ratio, scalar, threshold, C.byref(out)))
     return out.value
+
+
+# ------------------------------------------------------------------ operators (include/torpor_ops.h)
+
+TPO_WORK_BYTES = 32 << 20
+
+
+def tpo_w4_bytes(N: int, K: int, group: int, L=None):
+    """(code bytes, scale bytes) of the blocked order of an [N][K] matrix."""
+    L = L or lib()
+    c, s = C.c_uint64(), C.c_uint64()
+    _check(L, L.tpo_w4_bytes(N, K, group, C.byref(c), C.byref(s)))
+    return c.value, s.value
+
+
+def tpo_w4_pack(codes: np.ndarray, scales: np.ndarray, group: int, L=None):
+    """Plain order (codes uint8 [N][K/2], bf16 bits [N][K/group]) to blocked order: (uint8 codes, uint16 scales), flat."""
+    L = L or lib()
+    codes, scales = np.ascontiguousarray(codes, dtype=np.uint8), np.ascontiguousarray(scales, dtype=np.uint16)
+    if codes.ndim != 2 or scales.ndim != 2 or scales.shape[0] != codes.shape[0] or scales.shape[1] * group != 2 * codes.shape[1]:
+        raise ValueError(f"codes {codes.shape} and scales {scales.shape} do not belong together for groups of {group}")
+    n, k = codes.shape[0], 2 * codes.shape[1]
+    cb, sb = tpo_w4_bytes(n, k, group, L)
+    c, s = np.empty(cb, dtype=np.uint8), np.empty(sb // 2, dtype=np.uint16)
+    _check(L, L.tpo_w4_pack(codes.ctypes.data, scales.ctypes.data, n, k, group, c.ctypes.data, s.ctypes.data))
+    return c, s
+
+
+def tpo_w4_quantize(w: np.ndarray, group: int, L=None):
+    """fp32 [N][K] to the plain order: (codes uint8 [N][K/2], scales as bf16 bits [N][K/group])."""
+    L = L or lib()
+    w = np.ascontiguousarray(w, dtype=np.float32)
+    if w.ndim != 2:
+        raise ValueError(f"weights of {w.ndim} dimensions")
+    n, k = w.shape
+    tpo_w4_bytes(n, k, group, L)
+    codes, scales = np.empty((n, k // 2), dtype=np.uint8), np.empty((n, k // group), dtype=np.uint16)
+    _check(L, L.tpo_w4_quantize(w.ctypes.data, n, k, group, codes.ctypes.data, scales.ctypes.data))
+    return codes, scales
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, not on {device}")
+
+
+def _launch_on(device, stream):
+    """The raw stream of a call on `device`: the caller's, which must belong to it, or the device's current one."""
+    import torch
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device.index)
+    owner = getattr(stream, "device", None)
+    if owner is not None and owner != device:
+        raise ValueError(f"stream of {owner}, tensors on {device}")
+    return _ptr(stream)
+
+
+class W4Weight:
+    """A matrix W[N][K] in 4 bits on the device: codes (uint8) and scales (bf16) in blocked order."""
+
+    def __init__(self, codes, scales, out_features: int, in_features: int, group: int):
+        import torch
+        cb, sb = tpo_w4_bytes(out_features, in_features, group)
+        if codes.dtype != torch.uint8 or scales.dtype != torch.bfloat16:
+            raise ValueError(f"codes must be uint8 and scales bfloat16, not {codes.dtype} and {scales.dtype}")
+        if codes.numel() != cb or 2 * scales.numel() != sb:
+            raise ValueError(f"{codes.numel()} code bytes and {2 * scales.numel()} scale bytes, need {cb} and {sb}")
+        if not (codes.is_contiguous() and scales.is_contiguous()):
+            raise ValueError("codes and scales must be contiguous")
+        if codes.device.type != "cuda":
+            raise ValueError(f"codes on {codes.device}")
+        _same_device(codes.device, scales=scales)
+        self.codes, self.scales, self.device = codes, scales, codes.device
+        self.out_features, self.in_features, self.group = out_features, in_features, group
+
+    @classmethod
+    def from_plain(cls, codes: np.ndarray, scales: np.ndarray, group: int, device="cuda"):
+        """From the plain order in host memory (what tpo_w4_quantize gives and checkpoints hold)."""
+        import torch
+        c, s = tpo_w4_pack(codes, scales, group)
+        return cls(torch.from_numpy(c).to(device), torch.from_numpy(s.view(np.int16)).to(device).view(torch.bfloat16),
+                   codes.shape[0], 2 * codes.shape[1], group)
+
+
+def _rows(t, name, rows, cols, dtypes):
+    """Address and row stride of a [rows][cols] tensor whose rows are contiguous."""
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} is {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} is {tuple(t.shape)}, need {(rows, cols)}")
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    return t.data_ptr(), t.stride(0) if rows > 1 else cols + -cols % 8
+
+
+def tpo_linear_w4(x, weight: W4Weight, out, bias=None, res=None, act: str = "none", work=None, stream=None):
+    """out = act(x W^T + bias + res): x, res bf16 [M][K] and [M][N], out bf16 or fp32 [M][N], bias bf16 [N], all on the
+    weight's device. stream: a torch stream of that device (default: its current one); work: a uint8 tensor of scratch."""
+    import torch
+    bf = torch.bfloat16
+    n, k = weight.out_features, weight.in_features
+    _same_device(weight.device, x=x, out=out, bias=bias, res=res, work=work)
+    a = tpo_linear_w4_args()
+    m = x.shape[0]
+    a.x, a.ldx = _rows(x, "x", m, k, (bf,))
+    a.y, a.ldy = _rows(out, "out", m, n, (bf, torch.float32))
+    a.y_dtype = TP_BF16 if out.dtype == bf else TP_F32
+    a.wq, a.scales = weight.codes.data_ptr(), weight.scales.data_ptr()
+    if bias is not None:
+        if bias.dtype != bf or bias.shape != (n,) or not bias.is_contiguous():
+            raise ValueError(f"bias must be a contiguous bfloat16 [{n}]")
+        a.bias = bias.data_ptr()
+    if res is not None:
+        a.res, a.ldr = _rows(res, "res", m, n, (bf,))
+    a.M, a.N, a.K, a.group, a.act = m, n, k, weight.group, TP_ACT[act]
+    if work is not None:
+        a.work, a.work_bytes = work.data_ptr(), work.numel() * work.element_size()
+    L = _lib or lib()
+    status = L.tpo_linear_w4(a, _launch_on(weight.device, stream))
+    if status != TP_OK:
+        _check(L, status)
+
+
+def tpo_attention(q, k, v, out, q_lens=None, kv_lens=None, causal: bool = False, window=(-1, -1), sinks: int = 0,
+                  scale: float = 0.0, work=None, stream=None):
+    """Attention of q [B][q_len][heads][dim] over k, v [B][kv_len][kv_heads][dim] into out (as q), bf16, with any strides
+    but the last. q_lens, kv_lens: int32 [B] on the device; window: keys to the left and right of a query's
+    position that it sees (negative: all); sinks: first keys that it sees besides; see torpor_ops.h."""
+    import torch
+    if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape or out.shape != q.shape:
+        raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, out {tuple(out.shape)}")
+    b, nq, h, d = q.shape
+    if k.shape[0] != b or k.shape[3] != d:
+        raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)}")
+    dev = q.device
+    if dev.type != "cuda":
+        raise ValueError(f"q on {dev}")
+    _same_device(dev, k=k, v=v, out=out, q_lens=q_lens, kv_lens=kv_lens, work=work)
+    a = tpo_attention_args()
+    for name, t, st in (("q", q, a.q_stride), ("k", k, a.k_stride), ("v", v, a.v_stride), ("out", out, a.out_stride)):
+        if t.dtype != torch.bfloat16:
+            raise ValueError(f"{name} is {t.dtype}")
+        s0, s1, s2, s3 = t.stride()
+        if s3 != 1:
+            raise ValueError(f"{name}: the values of a head must be contiguous")
+        # the stride of a dimension of one entry is never used
+        n0, n1, n2, _ = t.shape
+        st[0], st[1], st[2] = s0 if n0 > 1 else 0, s1 if n1 > 1 else 0, s2 if n2 > 1 else 0
+    for name, t in (("q_lens", q_lens), ("kv_lens", kv_lens)):
+        if t is not None and (t.dtype != torch.int32 or t.shape != (b,) or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous int32 [{b}]")
+    a.q, a.k, a.v, a.out = q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr()
+    a.q_lens = None if q_lens is None else q_lens.data_ptr()
+    a.kv_lens = None if kv_lens is None else kv_lens.data_ptr()
+    a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len = b, h, k.shape[2], d, nq, k.shape[1]
+    a.causal, a.sinks, a.scale = int(causal), sinks, scale
+    a.window_left, a.window_right = window
+    if work is not None:
+        a.work, a.work_bytes = work.data_ptr(), work.numel() * work.element_size()
+    L = _lib or lib()
+    status = L.tpo_attention(a, _launch_on(dev, stream))
+    if status != TP_OK:
+        _check(L, status)
 
 
 _probe = None
