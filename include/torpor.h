@@ -43,15 +43,24 @@ enum {
   TP_E_STATE = -5    /* call not valid in the current state */
 };
 
-typedef enum { TP_F32 = 0, TP_BF16 = 1 } tp_dtype;
+/* TP_W4G*: the weight matrices of the linear layers in 4 bits with a bf16 scale for every 32, 64 or 128 columns of a row
+ * (torpor_ops.h), everything else as under TP_BF16 (bf16 inputs, biases, embeddings and LayerNorms). 3.2 to 3.9 times
+ * fewer bytes of those matrices cross the host link in a cold request. MLP and BERT models whose width, d and ffn are
+ * multiples of 128. */
+typedef enum { TP_F32 = 0, TP_BF16 = 1, TP_W4G32 = 2, TP_W4G64 = 3, TP_W4G128 = 4 } tp_dtype;
 
 /* Model families (dims[] meaning per family):
  *   TP_ARCH_MLP      {layers, width, act(TP_ACT_*)}; layers x Linear(width, width) + bias,
  *                    activation after every layer but the last.
  *   TP_ARCH_RESNET50 {classes, image}; ResNet-50 v1.5, batch-norm folded into conv
  *                    biases, NHWC input [B][image][image][3], image % 32 == 0.
- *   TP_ARCH_BERT     {layers, d, heads, ffn, seq, vocab, maxpos}; post-LN encoder,
- *                    head dim 64, token type 0, no mask, LN eps 1e-12. */
+ *   TP_ARCH_BERT     {layers, d, heads, ffn, seq, vocab, maxpos, attention}; post-LN encoder,
+ *                    head dim 64, token type 0, LN eps 1e-12. Without TP_BERT_ATTENTION in the last field: no mask,
+ *                    seq a multiple of 32 up to 256. With it: any seq up to 16384, and
+ *                    a sample is the token ids in front of its first negative one (padding), whose outputs alone
+ *                    mean anything: those of padding are finite. Every token attends to the tokens of
+ *                    its sample at most `window` (1..65535; 0: all) places away, and to the first `sinks` (0..16383). */
+#define TP_BERT_ATTENTION(window, sinks) ((int32_t)(0x40000000u | (uint32_t)(sinks) << 16 | (uint32_t)(window)))
 typedef enum { TP_ARCH_MLP = 0, TP_ARCH_RESNET50 = 1, TP_ARCH_BERT = 2 } tp_arch;
 enum { TP_ACT_NONE = 0, TP_ACT_RELU = 1, TP_ACT_GELU = 2 };
 
@@ -59,6 +68,8 @@ enum { TP_ACT_NONE = 0, TP_ACT_RELU = 1, TP_ACT_GELU = 2 };
  * the FC is the last layer). BERT: layer 0 holds the embeddings, layers 1..L the encoder. */
 enum {
   TP_ROLE_W = 0, TP_ROLE_B = 1,
+  /* the scales of the 4-bit matrices W, QKV_W, O_W, FFN1_W and FFN2_W */
+  TP_ROLE_W_SCALE = 2, TP_ROLE_QKV_SCALE = 3, TP_ROLE_O_SCALE = 4, TP_ROLE_FFN1_SCALE = 5, TP_ROLE_FFN2_SCALE = 6,
   TP_ROLE_TOK_EMB = 10, TP_ROLE_POS_EMB = 11, TP_ROLE_TYPE_EMB = 12,
   TP_ROLE_EMB_LN_G = 13, TP_ROLE_EMB_LN_B = 14,
   TP_ROLE_QKV_W = 20, TP_ROLE_QKV_B = 21, TP_ROLE_O_W = 22, TP_ROLE_O_B = 23,
@@ -68,12 +79,13 @@ enum {
 
 /* One tensor inside the host weight buffer. Linear weights are [out][in], conv weights
  * OHWI, the fused BERT QKV weight is [3d][d] with rows Q (heads x 64), K, V; LN gamma and
- * beta are separate [d] tensors. Unused shape entries are 0. */
+ * beta are separate [d] tensors. Unused shape entries are 0. A 4-bit matrix has the shape [out][in] and
+ * out * in / 2 bytes (codes in plain order, torpor_ops.h), its scales the shape [out][in / group] in bf16. */
 typedef struct {
   uint32_t layer;     /* first-use unit the tensor belongs to */
   uint32_t role;      /* TP_ROLE_* */
   uint64_t offset;    /* byte offset in the host buffer, multiple of 256 */
-  uint64_t bytes;     /* byte size = prod(shape) * element size */
+  uint64_t bytes;     /* byte size = prod(shape) * element size (4-bit codes: prod(shape) / 2) */
   int64_t shape[4];
 } tp_tensor_desc;
 
@@ -81,7 +93,7 @@ typedef struct {
  * decrease and offsets strictly increase; tensors do not overlap. */
 typedef struct {
   int32_t arch;        /* tp_arch */
-  int32_t dtype;       /* tp_dtype of every weight; BERT and ResNet require TP_BF16 */
+  int32_t dtype;       /* tp_dtype of every weight; ResNet requires TP_BF16, BERT that or TP_W4G* */
   int32_t dims[8];
   uint32_t n_tensors;
   const tp_tensor_desc* tensors;
@@ -339,7 +351,8 @@ TP_API tp_status tp_set_model_class(struct tp_ctx* ctx, int32_t model_id, int32_
 /* The library's pinned host image of a registered model (what a swap copies, byte for byte).
  * It equals the registered bytes except that bf16 MLP weight matrices whose width is a
  * multiple of 128 are stored blocked for the skinny-batch kernel: each block of 16 rows x
- * 128 columns is contiguous, ordered [32-column group][8-column slot][row][8 elements].
+ * 128 columns is contiguous, ordered [32-column group][8-column slot][row][8 elements]; and that
+ * 4-bit matrices and their scales are in the blocked order of torpor_ops.h, in as many bytes.
  * *ptr stays valid until the model is unregistered; read-only. */
 TP_API tp_status tp_model_host_image(struct tp_ctx* ctx, int32_t model_id, const void** ptr, uint64_t* bytes);
 

@@ -33,11 +33,21 @@ class _Weights:
         t = self.m.tensor(name)
         if tuple(t.shape) != tuple(shape):
             raise ValueError(f"{name}: layout shape {t.shape}, architecture needs {shape}")
+        if t.dtype == "w4":
+            return self._codes(t)
         return _widen(self.blob[t.offset:t.offset + t.nbytes], t.dtype, self.dt).reshape(shape)
+
+    def _codes(self, t):
+        """A 4-bit matrix: (code - 8) times the scale of its group of columns; the even column in the low half byte."""
+        b = self.blob[t.offset:t.offset + t.nbytes].reshape(t.shape[0], t.shape[1] // 2)
+        code = np.stack([b & 15, b >> 4], axis=-1).reshape(t.shape)
+        s = self.m.tensor(t.name + ".scale")
+        scale = _widen(self.blob[s.offset:s.offset + s.nbytes], s.dtype, self.dt).reshape(s.shape)
+        return (code.astype(self.dt) - 8) * np.repeat(scale, t.shape[1] // s.shape[1], axis=1)
 
 
 def _input(x: np.ndarray, model_dtype: str, dt) -> np.ndarray:
-    if model_dtype == "bf16" and x.dtype == np.uint16:
+    if model_dtype != "f32" and x.dtype == np.uint16:
         return _widen(x.reshape(-1).view(np.uint8), "bf16", dt).reshape(x.shape)
     return x.astype(dt)
 
@@ -93,7 +103,11 @@ def resnet50_forward(model, x, dt=np.float64):
 
 
 def bert_forward(model, ids, dt=np.float64):
-    """BERT encoder, post-LN, no attention mask, token type 0 everywhere, LN eps 1e-12."""
+    """BERT encoder, post-LN, token type 0 everywhere, LN eps 1e-12. No attention mask, or (dims "window" and "sinks"):
+    a sample ends at its first negative id, and a token attends to those of its sample at most `window` places away (0:
+    all) and to the first `sinks`; outputs behind a sample's end are zeros here."""
+    if "window" in model.dims:
+        return _bert_masked(model, ids, dt)
     dm = model.dims
     L, d, H, f, V, P = dm["layers"], dm["d"], dm["heads"], dm["ffn"], dm["vocab"], dm["maxpos"]
     eps = 1e-12
@@ -111,6 +125,36 @@ def bert_forward(model, ids, dt=np.float64):
         h = ops.layernorm(h + ops.linear(g, w(f"{p}.ffn2.w", (d, f)), w(f"{p}.ffn2.b", (d,))),
                           w(f"{p}.ln2.g", (d,)), w(f"{p}.ln2.b", (d,)), eps)
     return h
+
+
+def _bert_masked(model, ids, dt):
+    """Each sample by itself, at its own length."""
+    dm = model.dims
+    L, d, H, f, V, P = dm["layers"], dm["d"], dm["heads"], dm["ffn"], dm["vocab"], dm["maxpos"]
+    w, eps = _Weights(model, dt), 1e-12
+    out = np.zeros((*ids.shape, d), dtype=dt)
+    for i, row in enumerate(ids):
+        n = int(np.argmax(row < 0)) if (row < 0).any() else len(row)
+        if n == 0:
+            continue
+        far = np.abs(np.arange(n)[:, None] - np.arange(n)[None]) > (dm["window"] or n)
+        hidden = far & (np.arange(n) >= dm["sinks"])[None]
+        h = w("emb.tok", (V, d))[row[:n]] + w("emb.pos", (P, d))[:n] + w("emb.type", (2, d))[0]
+        h = ops.layernorm(h, w("emb.ln.g", (d,)), w("emb.ln.b", (d,)), eps)
+        for l in range(1, L + 1):
+            p = f"l{l}"
+            qkv = ops.linear(h, w(f"{p}.qkv.w", (3 * d, d)), w(f"{p}.qkv.b", (3 * d,)))
+            q, k, v = (qkv[:, j * d:(j + 1) * d].reshape(n, H, 64).transpose(1, 0, 2) for j in range(3))
+            s = q @ k.transpose(0, 2, 1) / 8
+            s[:, hidden] = -np.inf
+            a = (ops.softmax(s) @ v).transpose(1, 0, 2).reshape(n, d)
+            h = ops.layernorm(h + ops.linear(a, w(f"{p}.o.w", (d, d)), w(f"{p}.o.b", (d,))),
+                              w(f"{p}.ln1.g", (d,)), w(f"{p}.ln1.b", (d,)), eps)
+            g = ops.gelu(ops.linear(h, w(f"{p}.ffn1.w", (f, d)), w(f"{p}.ffn1.b", (f,))))
+            h = ops.layernorm(h + ops.linear(g, w(f"{p}.ffn2.w", (d, f)), w(f"{p}.ffn2.b", (d,))),
+                              w(f"{p}.ln2.g", (d,)), w(f"{p}.ln2.b", (d,)), eps)
+        out[i, :n] = h
+    return out
 
 
 def forward(model, x, dt=np.float64):

@@ -66,6 +66,12 @@ bool expected(const tp_model_desc* d, std::vector<Want>* w, uint32_t* n_layers, 
   auto add = [&](uint32_t l, uint32_t r, int64_t a, int64_t b = 0, int64_t c = 0, int64_t e = 0) {
     w->push_back({l, r, {a, b, c, e}});
   };
+  const int group = w4_group(d->dtype);
+  // a linear layer's matrix, in 4 bits with its scales
+  auto matrix = [&](uint32_t l, uint32_t r, int64_t out, int64_t in) {
+    add(l, r, out, in);
+    if (group) add(l, (uint32_t)scale_role(r), out, in / group);
+  };
   switch (d->arch) {
     case TP_ARCH_MLP: {
       const int L = D[0], W = D[1], act = D[2];
@@ -74,8 +80,12 @@ bool expected(const tp_model_desc* d, std::vector<Want>* w, uint32_t* n_layers, 
                    L, W, act);
         return false;
       }
-      if (d->dtype != TP_F32 && d->dtype != TP_BF16) { *err = "MLP dtype must be TP_F32 or TP_BF16"; return false; }
-      for (int l = 0; l < L; ++l) { add(l, TP_ROLE_W, W, W); add(l, TP_ROLE_B, W); }
+      if (d->dtype != TP_F32 && d->dtype != TP_BF16 && !group) {
+        *err = "MLP dtype must be TP_F32, TP_BF16 or TP_W4G*";
+        return false;
+      }
+      if (group && W % 128) { *err = fmt("MLP width %lld: 4-bit weights need a multiple of 128", W); return false; }
+      for (int l = 0; l < L; ++l) { matrix(l, TP_ROLE_W, W, W); add(l, TP_ROLE_B, W); }
       *n_layers = L;
       return true;
     }
@@ -96,21 +106,26 @@ bool expected(const tp_model_desc* d, std::vector<Want>* w, uint32_t* n_layers, 
     }
     case TP_ARCH_BERT: {
       const int L = D[0], dm = D[1], H = D[2], F = D[3], S = D[4], V = D[5], P = D[6];
-      if (L < 1 || H < 1 || dm != 64 * H || dm > 1024 || F < 8 || F % 8 || F > 16384 || S < 32 || S % 32 ||
-          S > 256 || P < S || V < 1) {
+      const bool masked = bert_attention(D).on;
+      if (L < 1 || H < 1 || dm != 64 * H || dm > 1024 || F < 8 || F % 8 || F > 16384 || P < S || V < 1 ||
+          (masked ? S < 1 || S > 16384 : S < 32 || S % 32 || S > 256)) {
         *err = "BERT dims {layers, d, heads, ffn, seq, vocab, maxpos}: need d == 64*heads <= 1024, "
-               "ffn%8==0, seq%32==0, 32<=seq<=256, maxpos>=seq, vocab>=1";
+               "ffn%8==0, seq%32==0, 32<=seq<=256 (with TP_BERT_ATTENTION 1<=seq<=16384), maxpos>=seq, vocab>=1";
         return false;
       }
-      if (d->dtype != TP_BF16) { *err = "BERT dtype must be TP_BF16"; return false; }
+      if (d->dtype != TP_BF16 && !group) { *err = "BERT dtype must be TP_BF16 or TP_W4G*"; return false; }
+      if (group && (dm % 128 || F % 128)) {
+        *err = fmt("BERT d %lld, ffn %lld: 4-bit weights need multiples of 128", dm, F);
+        return false;
+      }
       add(0, TP_ROLE_TOK_EMB, V, dm); add(0, TP_ROLE_POS_EMB, P, dm); add(0, TP_ROLE_TYPE_EMB, 2, dm);
       add(0, TP_ROLE_EMB_LN_G, dm); add(0, TP_ROLE_EMB_LN_B, dm);
       for (int l = 1; l <= L; ++l) {
-        add(l, TP_ROLE_QKV_W, 3 * dm, dm); add(l, TP_ROLE_QKV_B, 3 * dm);
-        add(l, TP_ROLE_O_W, dm, dm); add(l, TP_ROLE_O_B, dm);
+        matrix(l, TP_ROLE_QKV_W, 3 * dm, dm); add(l, TP_ROLE_QKV_B, 3 * dm);
+        matrix(l, TP_ROLE_O_W, dm, dm); add(l, TP_ROLE_O_B, dm);
         add(l, TP_ROLE_LN1_G, dm); add(l, TP_ROLE_LN1_B, dm);
-        add(l, TP_ROLE_FFN1_W, F, dm); add(l, TP_ROLE_FFN1_B, F);
-        add(l, TP_ROLE_FFN2_W, dm, F); add(l, TP_ROLE_FFN2_B, dm);
+        matrix(l, TP_ROLE_FFN1_W, F, dm); add(l, TP_ROLE_FFN1_B, F);
+        matrix(l, TP_ROLE_FFN2_W, dm, F); add(l, TP_ROLE_FFN2_B, dm);
         add(l, TP_ROLE_LN2_G, dm); add(l, TP_ROLE_LN2_B, dm);
       }
       *n_layers = L + 1;
@@ -138,6 +153,7 @@ tp_status validate_model(const tp_model_desc* d, uint64_t host_bytes, ModelSpec*
   ModelSpec m;
   m.arch = d->arch;
   m.dtype = d->dtype;
+  m.group = w4_group(d->dtype);
   std::copy(d->dims, d->dims + 8, m.dims);
   m.n_layers = n_layers;
   m.lookup.assign((size_t)n_layers * ModelSpec::kRoles, -1);
@@ -180,9 +196,10 @@ tp_status validate_model(const tp_model_desc* d, uint64_t host_bytes, ModelSpec*
       }
       if (w.shape[k]) n *= (uint64_t)w.shape[k];
     }
-    if (t.bytes != n * esz) {
+    const uint64_t need = m.group && scale_role(w.role) >= 0 ? n / 2 : n * esz;
+    if (t.bytes != need) {
       *err = fmt("tensor (layer %lld, role %lld): %lld bytes, shape needs %lld", w.layer, w.role,
-                 (long long)t.bytes, (long long)(n * esz));
+                 (long long)t.bytes, (long long)need);
       return TP_E_INVAL;
     }
   }
@@ -310,8 +327,8 @@ std::vector<double> layer_cost_us(const ModelSpec& m, int32_t batch) {
   std::vector<double> t(m.n_layers, 0.0);
   switch (m.arch) {
     case TP_ARCH_MLP: {
-      const double W = m.dims[1], esz = m.dtype == TP_F32 ? 4 : 2;
-      for (auto& v : t) v = kernel_us(2 * B * W * W, W * W * esz + 2 * B * W * esz);
+      const double W = m.dims[1], esz = m.dtype == TP_F32 ? 4 : 2, wsz = m.group ? 0.5 + 2.0 / m.group : esz;
+      for (auto& v : t) v = kernel_us(2 * B * W * W, W * W * wsz + 2 * B * W * esz);
       break;
     }
     case TP_ARCH_RESNET50: {
@@ -336,14 +353,17 @@ std::vector<double> layer_cost_us(const ModelSpec& m, int32_t batch) {
     }
     case TP_ARCH_BERT: {
       const double d = m.dims[1], F = m.dims[3], S = m.dims[4], M = B * S;
-      t[0] = kernel_us(0, M * d * 8);
+      const double wsz = m.group ? 0.5 + 2.0 / m.group : 2;                             // bytes of a weight
+      const BertAttention at = bert_attention(m.dims);
+      const double keys = at.on && at.window ? std::min(S, 2.0 * at.window + 1 + at.sinks) : S;
+      t[0] = kernel_us(0, M * d * 8) + (at.on ? kernel_us(0, M * 4) : 0);
       for (size_t l = 1; l < t.size(); ++l)
-        t[l] = kernel_us(2 * M * d * 3 * d, 2 * (3 * d * d + M * d + 3 * M * d)) +        // QKV
-               kernel_us(4 * B * S * S * d, 2 * (3 * M * d + M * d)) +                    // attention
-               kernel_us(2 * M * d * d, 2 * (d * d + M * d) + 8 * M * d) +                 // O + residual
+        t[l] = kernel_us(2 * M * d * 3 * d, wsz * 3 * d * d + 2 * (M * d + 3 * M * d)) +   // QKV
+               kernel_us(4 * B * S * keys * d, 2 * (3 * M * d + M * d)) +                 // attention
+               kernel_us(2 * M * d * d, wsz * d * d + 2 * M * d + 8 * M * d) +             // O + residual
                kernel_us(0, 6 * M * d) +                                                 // LN
-               kernel_us(2 * M * d * F, 2 * (d * F + M * d + M * F)) +                   // FFN1
-               kernel_us(2 * M * F * d, 2 * (d * F + M * F) + 8 * M * d) +               // FFN2 + residual
+               kernel_us(2 * M * d * F, wsz * d * F + 2 * (M * d + M * F)) +             // FFN1
+               kernel_us(2 * M * F * d, wsz * d * F + 2 * M * F + 8 * M * d) +           // FFN2 + residual
                kernel_us(0, 6 * M * d);                                                  // LN
       break;
     }
@@ -376,7 +396,7 @@ std::vector<Chunk> plan_chunks_cost(const ModelSpec& m, int32_t batch, const Lin
 }
 
 uint64_t workspace_bytes(const ModelSpec& m, int32_t batch) {
-  return activation_bytes(m, batch) + (m.dtype == TP_BF16 ? kSplitScratch : 0);
+  return activation_bytes(m, batch) + (m.dtype != TP_F32 ? kSplitScratch : 0);
 }
 
 uint64_t activation_bytes(const ModelSpec& m, int32_t batch) {
@@ -397,7 +417,7 @@ uint64_t activation_bytes(const ModelSpec& m, int32_t batch) {
     case TP_ARCH_BERT: {
       const uint64_t M = B * m.dims[4], d = m.dims[1], F = m.dims[3];
       return round_up(M * d * 2, 256) * 2 + round_up(M * 3 * d * 2, 256) + round_up(M * d * 4, 256) +
-             round_up(M * F * 2, 256);
+             round_up(M * F * 2, 256) + (bert_attention(m.dims).on ? round_up(B * 4, 256) : 0);
     }
   }
   return 0;

@@ -39,12 +39,41 @@ struct ModelSpec {
   uint32_t n_layers = 0;
   std::vector<int32_t> lookup;  // (layer * kRoles + role) -> tensor index, -1 if absent
   static constexpr int kRoles = 32;
+  int32_t group = 0;            // columns per scale of the 4-bit matrices, 0: there are none
   bool packed_mlp = false;      // bf16 MLP weights stored in 16 x 128 blocks (see pack_rows16x128)
 
   const tp_tensor_desc& t(uint32_t layer, uint32_t role) const {
     return tensors[lookup[layer * kRoles + role]];
   }
 };
+
+// Columns per scale of a dtype with 4-bit matrices, else 0.
+inline int32_t w4_group(int32_t dtype) {
+  return dtype == TP_W4G32 ? 32 : dtype == TP_W4G64 ? 64 : dtype == TP_W4G128 ? 128 : 0;
+}
+
+// The last field of a BERT's dims (TP_BERT_ATTENTION), taken apart.
+struct BertAttention {
+  bool on = false;
+  int32_t window = 0, sinks = 0;
+};
+inline BertAttention bert_attention(const int32_t* dims) {
+  const uint32_t f = (uint32_t)dims[7];
+  if (f >> 30 != 1) return {};
+  return {true, (int32_t)(f & 0xffff), (int32_t)(f >> 16 & 0x3fff)};
+}
+
+// The scale's role of a 4-bit matrix's role, -1 for a role that is never held in 4 bits.
+inline int32_t scale_role(uint32_t role) {
+  switch (role) {
+    case TP_ROLE_W: return TP_ROLE_W_SCALE;
+    case TP_ROLE_QKV_W: return TP_ROLE_QKV_SCALE;
+    case TP_ROLE_O_W: return TP_ROLE_O_SCALE;
+    case TP_ROLE_FFN1_W: return TP_ROLE_FFN1_SCALE;
+    case TP_ROLE_FFN2_W: return TP_ROLE_FFN2_SCALE;
+    default: return -1;
+  }
+}
 
 // Validates `d` against its family (see torpor.h) and fills `out`. Returns TP_OK or
 // TP_E_INVAL with a message in *err.
@@ -86,7 +115,7 @@ std::vector<Chunk> plan_chunks_cost(const ModelSpec& m, int32_t batch, const Lin
 // Activation buffers of the executors for `batch` samples (each buffer 256-aligned).
 uint64_t activation_bytes(const ModelSpec& m, int32_t batch);
 
-// fp32 partial tiles for contractions split over k (bf16 families only); placed after
+// fp32 partial tiles for contractions split over k (not the fp32 family); placed after
 // the activation buffers.
 constexpr uint64_t kSplitScratch = 32ull << 20;
 

@@ -19,6 +19,32 @@ namespace tp {
     if (e_ != hipSuccess) return e_;       \
   } while (0)
 
+namespace {
+
+// The 4-bit linear layer of a model: y[M][N] = act(x[M][K] W^T + b (+ res)), matrix, scales and bias by their roles.
+hipError_t model_linear_w4(ExecCtx& x, uint32_t layer, uint32_t w_role, uint32_t b_role, const uint16_t* in, int M, int act,
+                           const uint16_t* res, void* out, bool out_f32) {
+  const tp_tensor_desc& t = x.m->spec.t(layer, w_role);
+  k::LinearW4 a;
+  a.x = in;
+  a.wq = x.t<uint8_t>(layer, w_role);
+  a.scales = x.t<uint16_t>(layer, (uint32_t)scale_role(w_role));
+  a.bias = x.t<uint16_t>(layer, b_role);
+  a.res = res;
+  a.y = out;
+  a.y_f32 = out_f32;
+  a.M = M;
+  a.N = (int)t.shape[0];
+  a.K = (int)t.shape[1];
+  a.ldx = a.K;
+  a.ldy = a.ldr = a.N;
+  a.group = x.m->spec.group;
+  a.act = act;
+  return k::linear_w4(a, x.split, x.stream);
+}
+
+}  // namespace
+
 hipError_t run_mlp(ExecCtx& x) {
   const ModelSpec& s = x.m->spec;
   const int L = s.dims[0], W = s.dims[1], act = s.dims[2], B = x.batch;
@@ -26,9 +52,9 @@ hipError_t run_mlp(ExecCtx& x) {
   const uint64_t bytes = round_up((uint64_t)B * W * (f32 ? 4 : 2), 256);
   char* buf[2] = {x.work, x.work + bytes};
   const void* cur = x.in;
-  if (!f32 && B > k::kSkinnyRows && ((uintptr_t)x.in & 15)) {
-    // the tiled contraction reads its input from 16-byte boundaries only: an input elsewhere is copied
-    // into the second buffer, which layer 0 does not write
+  if (!f32 && (s.group || B > k::kSkinnyRows) && ((uintptr_t)x.in & 15)) {
+    // the tiled contraction and the 4-bit one read their input from 16-byte boundaries only: an input elsewhere is
+    // copied into the second buffer, which layer 0 does not write
     TP_TRY(k::copy_aligned(static_cast<const uint16_t*>(x.in), (uint64_t)B * W, reinterpret_cast<uint16_t*>(buf[1]),
                            x.stream));
     cur = buf[1];
@@ -41,6 +67,8 @@ hipError_t run_mlp(ExecCtx& x) {
     if (f32) {
       TP_TRY(k::linear_f32(static_cast<const float*>(cur), B, W, x.t<float>(l, TP_ROLE_W), W,
                            x.t<float>(l, TP_ROLE_B), a, static_cast<float*>(dst), x.far(), x.stream));
+    } else if (s.group) {
+      TP_TRY(model_linear_w4(x, l, TP_ROLE_W, TP_ROLE_B, static_cast<const uint16_t*>(cur), B, a, nullptr, dst, last));
     } else {
       k::Epilogue ep;
       ep.bias = x.t<uint16_t>(l, TP_ROLE_B);
@@ -173,18 +201,59 @@ hipError_t run_bert(ExecCtx& x) {
   float* pre = reinterpret_cast<float*>(take((uint64_t)M * d * 4));
   uint16_t* ff = reinterpret_cast<uint16_t*>(take((uint64_t)M * F * 2));
 
+  // lengths in front of the padding, and attention with them, the window and the sinks
+  const BertAttention masked = bert_attention(s.dims);
+  int32_t* lens = masked.on ? reinterpret_cast<int32_t*>(take((uint64_t)B * 4)) : nullptr;
+  k::Attention at;
+  if (masked.on) {
+    TP_TRY(k::seq_lengths(static_cast<const int32_t*>(x.in), B, S, lens, x.stream));
+    at.q = qkv;
+    at.k = qkv + d;
+    at.v = qkv + 2 * d;
+    at.out = att;
+    for (int64_t* st : {at.qs, at.ks, at.vs}) {
+      st[0] = (int64_t)S * 3 * d;
+      st[1] = 3 * d;
+      st[2] = 64;
+    }
+    at.os[0] = (int64_t)S * d;
+    at.os[1] = d;
+    at.os[2] = 64;
+    at.q_lens = at.kv_lens = lens;
+    at.batch = B;
+    at.heads = at.kv_heads = H;
+    at.dim = 64;
+    at.q_len = at.kv_len = S;
+    if (masked.window) at.left = at.right = masked.window;
+    at.sinks = masked.sinks;
+    at.scale = 0.125f;
+    at.zero_tail = 1;       // the rows of padding go on through the layer: defined values, not what the buffer held
+  }
+
   TP_TRY(x.wait->need(0));
   TP_TRY(k::embed_ln(static_cast<const int32_t*>(x.in), M, S, d, V, x.t<uint16_t>(0, TP_ROLE_TOK_EMB),
                      x.t<uint16_t>(0, TP_ROLE_POS_EMB), x.t<uint16_t>(0, TP_ROLE_TYPE_EMB),
                      x.t<uint16_t>(0, TP_ROLE_EMB_LN_G), x.t<uint16_t>(0, TP_ROLE_EMB_LN_B), eps, h, x.stream));
   for (int l = 1; l <= L; ++l) {
     TP_TRY(x.wait->need(l));
+    const bool last = l == L;
+    if (s.group) {
+      TP_TRY(model_linear_w4(x, l, TP_ROLE_QKV_W, TP_ROLE_QKV_B, h, M, k::ACT_NONE, nullptr, qkv, false));
+      TP_TRY(masked.on ? k::attention_masked(at, x.split, x.stream) : k::attention(qkv, B, S, H, att, x.stream));
+      TP_TRY(model_linear_w4(x, l, TP_ROLE_O_W, TP_ROLE_O_B, att, M, k::ACT_NONE, h, pre, true));
+      TP_TRY(k::layernorm(pre, M, d, x.t<uint16_t>(l, TP_ROLE_LN1_G), x.t<uint16_t>(l, TP_ROLE_LN1_B), eps, h, 0, x.stream));
+      TP_TRY(model_linear_w4(x, l, TP_ROLE_FFN1_W, TP_ROLE_FFN1_B, h, M, k::ACT_GELU, nullptr, ff, false));
+      TP_TRY(model_linear_w4(x, l, TP_ROLE_FFN2_W, TP_ROLE_FFN2_B, ff, M, k::ACT_NONE, h, pre, true));
+      TP_TRY(k::layernorm(pre, M, d, x.t<uint16_t>(l, TP_ROLE_LN2_G), x.t<uint16_t>(l, TP_ROLE_LN2_B), eps,
+                          last ? x.out : static_cast<void*>(h), last, x.stream));
+      continue;
+    }
     k::Epilogue e1;
     e1.w_far = x.far();
     e1.bias = x.t<uint16_t>(l, TP_ROLE_QKV_B);
     e1.out = qkv;
     TP_TRY(k::linear_bf16(h, M, d, x.t<uint16_t>(l, TP_ROLE_QKV_W), 3 * d, e1, x.split, x.stream));
-    TP_TRY(k::attention(qkv, B, S, H, att, x.stream));
+    TP_TRY(masked.on ? k::attention_masked(at, x.split, x.stream) : k::attention(qkv, B, S, H, att, x.stream));
     k::Epilogue e2;
     e2.w_far = x.far();
     e2.bias = x.t<uint16_t>(l, TP_ROLE_O_B);
@@ -208,7 +277,6 @@ hipError_t run_bert(ExecCtx& x) {
     e4.res = h;
     e4.out = pre;
     e4.out_f32 = 1;
-    const bool last = l == L;
     e4.ln_g = x.t<uint16_t>(l, TP_ROLE_LN2_G);
     e4.ln_b = x.t<uint16_t>(l, TP_ROLE_LN2_B);
     e4.ln_eps = eps;

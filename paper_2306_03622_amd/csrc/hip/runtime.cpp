@@ -12,6 +12,7 @@
 #include <hip/hip_ext.h>
 
 #include "../core/errors.hpp"
+#include "../core/w4.hpp"
 #include "../kernels/kernels.hpp"
 #include "../kernels/touch.hpp"
 #include "scratch.hpp"
@@ -83,7 +84,7 @@ void destroy_streams(tp_ctx* c) {
 
 k::Split make_split(char* work, const Model* m, int batch) {
   k::Split sp;
-  if (m->spec.dtype != TP_BF16) return sp;
+  if (m->spec.dtype == TP_F32) return sp;
   sp.partials = reinterpret_cast<float*>(work + activation_bytes(m->spec, batch));
   sp.partial_bytes = kSplitScratch;
   return sp;
@@ -312,7 +313,7 @@ long forward_rows(const ModelSpec& s, int batch) {
 int forward_launches(const ModelSpec& s) {
   switch (s.arch) {
     case TP_ARCH_MLP: return s.dims[0];
-    case TP_ARCH_BERT: return 7 * s.dims[0] + 1;
+    case TP_ARCH_BERT: return 7 * s.dims[0] + 1 + bert_attention(s.dims).on;
     default: return 1 << 20;      // ResNet-50: > 50 convolutions
   }
 }
@@ -848,6 +849,26 @@ tp_status tp_register_model(tp_ctx* c, const tp_model_desc* desc, const void* ho
           const tp_tensor_desc& t = m->spec.t(l, TP_ROLE_W);
           pack_rows16x128(reinterpret_cast<const uint16_t*>(static_cast<const char*>(host_weights) + t.offset),
                           reinterpret_cast<uint16_t*>(static_cast<char*>(m->host) + t.offset), W, W);
+        }
+      });
+    for (auto& t : th) t.join();
+  }
+  if (m->spec.group) {
+    // 4-bit matrices and their scales in blocked order (no padding: whole 16 rows and 128 columns), tensors by turns
+    std::vector<std::thread> th;
+    for (uint32_t w = 0; w < 8; ++w)
+      th.emplace_back([&, w] {
+        for (uint32_t i = w; i < m->spec.tensors.size(); i += 8) {
+          const tp_tensor_desc& t = m->spec.tensors[i];
+          const int32_t sr = scale_role(t.role);
+          if (sr < 0) continue;
+          const tp_tensor_desc& sc = m->spec.t(t.layer, (uint32_t)sr);
+          const char* src = static_cast<const char*>(host_weights);
+          char* dst = static_cast<char*>(m->host);
+          w4_pack_codes(reinterpret_cast<const uint8_t*>(src + t.offset), t.shape[0], t.shape[1],
+                        reinterpret_cast<uint8_t*>(dst + t.offset));
+          w4_pack_scales(reinterpret_cast<const uint16_t*>(src + sc.offset), t.shape[0], t.shape[1], m->spec.group,
+                         reinterpret_cast<uint16_t*>(dst + sc.offset));
         }
       });
     for (auto& t : th) t.join();

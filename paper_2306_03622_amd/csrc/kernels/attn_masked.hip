@@ -411,7 +411,31 @@ hipError_t go(AttnArgs g, hipStream_t s) {
   return launch((k_attention_join<D>), dim3((unsigned)((slots + 3) / 4)), dim3(256), 0, s, g);
 }
 
+// A wave per sequence, four ids a lane and step.
+__global__ __launch_bounds__(256) void k_seq_lengths(const int32_t* __restrict__ ids, int B, int S, int32_t* __restrict__ lens) {
+  const int lane = threadIdx.x & 63, b = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (b >= B) return;
+  const int32_t* row = ids + (int64_t)b * S;
+  int first = S;
+  for (int s0 = 0; s0 < S && first == S; s0 += 256) {
+    int at = S;
+#pragma unroll
+    for (int i = 3; i >= 0; --i) {
+      const int s = s0 + 64 * i + lane;
+      const unsigned long long neg = __ballot(s < S && row[min(s, S - 1)] < 0);
+      if (neg) at = s0 + 64 * i + __builtin_ctzll(neg);
+    }
+    first = at;
+  }
+  if (lane == 0) lens[b] = first;
+}
+
 }  // namespace
+
+hipError_t seq_lengths(const int32_t* ids, int B, int S, int32_t* lens, hipStream_t s) {
+  if (!ids || !lens || B < 1 || S < 1) return hipErrorInvalidValue;
+  return launch(k_seq_lengths, dim3((B + 3) / 4), dim3(256), 0, s, ids, B, S, lens);
+}
 
 hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) {
   if (!a.q || !a.out || (a.kv_len > 0 && (!a.k || !a.v)) || a.batch < 1 || a.q_len < 1 || a.kv_len < 0 || a.kv_heads < 1 || a.heads < 1 ||

@@ -131,6 +131,9 @@ struct Attention {
 };
 hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s);
 
+// lens[b] = the number of ids of row b in front of its first negative one; ids [B][S].
+hipError_t seq_lengths(const int32_t* ids, int B, int S, int32_t* lens, hipStream_t s);
+
 // dst = src, n bf16 values (n % 8 == 0): dst 16-byte aligned, src at any element.
 hipError_t copy_aligned(const uint16_t* src, uint64_t n, uint16_t* dst, hipStream_t s);
 

@@ -21,7 +21,7 @@ HOST_LIB_PATH = os.path.join(_HERE, "libtorpor_host.so")
 PROBE_LIB_PATH = os.path.join(_HERE, "libtorpor_probe.so")
 
 TP_OK, TP_E_INVAL, TP_E_NOENT, TP_E_NOSPC, TP_E_HIP, TP_E_STATE = 0, -1, -2, -3, -4, -5
-TP_F32, TP_BF16 = 0, 1
+TP_F32, TP_BF16, TP_W4G32, TP_W4G64, TP_W4G128 = 0, 1, 2, 3, 4
 TP_ARCH_MLP, TP_ARCH_RESNET50, TP_ARCH_BERT = 0, 1, 2
 TP_ACT = {"none": 0, "relu": 1, "gelu": 2}
 TP_COPY_MEMCPY, TP_COPY_GATHER, TP_COPY_PAGEABLE, TP_COPY_ZERO = 0, 1, 2, 3
@@ -34,7 +34,7 @@ TP_CLASS_AUTO, TP_CLASS_LIGHT, TP_CLASS_HEAVY = 0, 1, 2
 TP_ALLOC_FIRST_FIT, TP_ALLOC_PARTITION, TP_ALLOC_PARTITION_CONSOLIDATE = 0, 1, 2
 TP_QUEUE_FIFO, TP_QUEUE_SLO = 0, 1
 ROLES = {
-    "w": 0, "b": 1,
+    "w": 0, "b": 1, "w_scale": 2, "qkv_scale": 3, "o_scale": 4, "ffn1_scale": 5, "ffn2_scale": 6,
     "tok_emb": 10, "pos_emb": 11, "type_emb": 12, "emb_ln_g": 13, "emb_ln_b": 14,
     "qkv_w": 20, "qkv_b": 21, "o_w": 22, "o_b": 23, "ln1_g": 24, "ln1_b": 25,
     "ffn1_w": 26, "ffn1_b": 27, "ffn2_w": 28, "ffn2_b": 29, "ln2_g": 30, "ln2_b": 31,
@@ -46,7 +46,14 @@ DEFAULT_CHUNK = 8 << 20
 # latency costs more than direct reads
 DEFAULT_DIRECT = 2 << 20
 ARCHS = {"mlp": TP_ARCH_MLP, "resnet50": TP_ARCH_RESNET50, "bert": TP_ARCH_BERT}
-DTYPES = {"f32": TP_F32, "bf16": TP_BF16}
+DTYPES = {"f32": TP_F32, "bf16": TP_BF16, "w4g32": TP_W4G32, "w4g64": TP_W4G64, "w4g128": TP_W4G128}
+
+
+def tp_bert_attention(window: int = 0, sinks: int = 0) -> int:
+    """The `attention` field of a BERT's dims (TP_BERT_ATTENTION): padding by negative ids, a window (0: all) and sinks."""
+    if not (0 <= window <= 65535 and 0 <= sinks <= 16383):
+        raise ValueError(f"window {window} or sinks {sinks} out of range")
+    return 0x40000000 | sinks << 16 | window
 
 
 class tp_tensor_desc(C.Structure):
@@ -282,7 +289,8 @@ class ModelDesc:
         elif model.arch == "resnet50":
             dims = [d["classes"], d["image"]]
         else:
-            dims = [d["layers"], d["d"], d["heads"], d["ffn"], d["seq"], d["vocab"], d["maxpos"]]
+            dims = [d["layers"], d["d"], d["heads"], d["ffn"], d["seq"], d["vocab"], d["maxpos"],
+                    d.get("attention", 0)]
         return cls(model.arch, model.dtype, dims,
                    [(t.layer, t.role, t.offset, t.nbytes, t.shape) for t in model.tensors])
 

@@ -50,8 +50,8 @@ class Tensor:
     layer: int
     role: str
     shape: tuple
-    dtype: str            # "f32" | "bf16"
-    init: tuple           # ("normal", std) | ("const", value)
+    dtype: str            # "f32" | "bf16" | "w4" (4-bit codes, two columns a byte)
+    init: tuple           # ("normal", std) | ("const", value) | ("about", value): value times 0.75 to 1.25
     offset: int = 0
 
     @property
@@ -60,13 +60,13 @@ class Tensor:
 
     @property
     def nbytes(self) -> int:
-        return self.numel * (4 if self.dtype == "f32" else 2)
+        return self.numel // 2 if self.dtype == "w4" else self.numel * (4 if self.dtype == "f32" else 2)
 
 
 @dataclass
 class Model:
     arch: str                      # "mlp" | "resnet50" | "bert"
-    dtype: str                     # "f32" | "bf16"
+    dtype: str                     # "f32" | "bf16" | "w4g32" | "w4g64" | "w4g128"
     dims: dict
     tensors: list = field(default_factory=list)
     total_bytes: int = 0
@@ -103,9 +103,15 @@ class Model:
             if kind == "normal":
                 x = rng.standard_normal(t.numel, dtype=np.float32)
                 x *= np.float32(val)
+            elif kind == "about":
+                x = (rng.random(t.numel, dtype=np.float32) * np.float32(0.5) + np.float32(0.75)) * np.float32(val)
             else:
                 x = np.full(t.numel, val, dtype=np.float32)
-            raw = bf16_round(x).view(np.uint8) if t.dtype == "bf16" else x.view(np.uint8)
+            if t.dtype == "w4":
+                code = (np.clip(np.rint(x), -8, 7) + 8).astype(np.uint8)
+                raw = code[0::2] | code[1::2] << 4
+            else:
+                raw = bf16_round(x).view(np.uint8) if t.dtype == "bf16" else x.view(np.uint8)
             buf[t.offset:t.offset + t.nbytes] = raw
             del x, raw
         return buf
@@ -210,6 +216,25 @@ def bert(seed: int, layers: int = 12, d: int = 768, heads: int = 12, ffn: int = 
         T(Tensor(f"{p}.ln2.b", l, "ln2_b", (d,), "bf16", ("const", 0.0)))
     m._pack()
     return m
+
+
+W4_STEPS = 2.6        # standard deviation of the codes of a 4-bit matrix
+
+
+def quantised(m: Model, group: int) -> Model:
+    """The MLP or BERT `m` with its weight matrices in 4 bits: codes N(0, W4_STEPS^2) rounded to -8..7, a scale per
+    `group` columns about the matrix's standard deviation / W4_STEPS."""
+    q = Model(m.arch, f"w4g{group}", dict(m.dims), seed=m.seed)
+    for t in m.tensors:
+        if t.role in ("w", "qkv_w", "o_w", "ffn1_w", "ffn2_w"):
+            q.tensors.append(Tensor(t.name, t.layer, t.role, t.shape, "w4", ("normal", W4_STEPS)))
+            role = "w_scale" if t.role == "w" else t.role[:-2] + "_scale"
+            q.tensors.append(Tensor(f"{t.name}.scale", t.layer, role, (t.shape[0], t.shape[1] // group), "bf16",
+                                    ("about", t.init[1] / W4_STEPS)))
+        else:
+            q.tensors.append(Tensor(t.name, t.layer, t.role, t.shape, t.dtype, t.init))
+    q._pack()
+    return q
 
 
 def config_model(cfg: int, seed: int | None = None) -> Model:
