@@ -52,7 +52,7 @@ TP_API tp_status tpo_w4_quantize(const float* w, int32_t N, int32_t K, int32_t g
 /* y[m][n] = act(sum_k x[m][k] W[n][k] + bias[n] + res[m][n]), m < M, n < N.
  * x, res bf16, y bf16 or fp32 (y_dtype), rows ldx, ldr and ldy elements apart; bias bf16 or NULL, res or NULL. Products
  * and sums are exact bf16 products in fp32 sums, scales applied to each group's sum, one rounding at the end.
- * x starts at a 16-byte boundary and ldx is a multiple of 8; wq and scales start at 16-byte boundaries. y may
+ * x starts at a 16-byte boundary and ldx is a multiple of 8 below 2^23; wq and scales start at 16-byte boundaries. y may
  * be res (same ldr and ldy, both bf16); apart from that outputs do not overlap inputs. M = 0 does nothing. An infinite
  * x[m][k] makes row m NaN. */
 typedef struct {

@@ -73,7 +73,7 @@ tp_status tpo_linear_w4(const tpo_linear_w4_args* a, void* stream) {
   if ((uintptr_t)a->y % (a->y_dtype == TP_F32 ? 4 : 2) || (uintptr_t)a->bias % 2 || (uintptr_t)a->res % 2)
     return inval(who, "y, bias or res not aligned to its element");
   if (a->ldx < a->K || a->ldy < a->N || (a->res && a->ldr < a->N)) return inval(who, "a row stride below the row's length");
-  if (a->ldx > kMostStride || a->ldy > kMostStride || (a->res && a->ldr > kMostStride)) return inval(who, "row stride too large");
+  if (a->ldx >= 1 << 23 || a->ldy > kMostStride || (a->res && a->ldr > kMostStride)) return inval(who, "row stride too large");
   if (a->res == a->y && (a->y_dtype != TP_BF16 || a->ldr != a->ldy))
     return inval(who, "y may be res only in bf16 and with the same row stride");
   k::LinearW4 g;

@@ -10,8 +10,8 @@
 //
 // Operand convention of the other contractions: A operand 16 weight rows, B operand 16 activation
 // rows, accumulator register e of lane l holds D[n = 4 (l / 16) + e][m = l % 16].
-#include "common.hpp"
-#include "kernels.hpp"
+#include "gemm_tile.hpp"
+#include "w4_plan.hpp"
 
 namespace tp {
 namespace k {
@@ -33,12 +33,21 @@ struct PtrFields<W4Args> {
 
 namespace {
 
-// eight codes as bf16 16 + c, column order
-__device__ __forceinline__ bf16x8 w4_values(uint32_t w) {
-  constexpr uint32_t mask = 0x00780078u, one = 0x41804180u;
-  return as_bf16x8(make_uint4(((w << 3) & mask) | one, ((w >> 1) & mask) | one, ((w >> 5) & mask) | one,
-                              ((w >> 9) & mask) | one));
-}
+// The two constants of the unpacking, in registers that the compiler knows nothing about: with literals it takes two
+// instructions for (x & mask) | one, a third more of the tiled kernel's. (The instruction itself is left to the compiler, which
+// keeps its distance from matrix instructions that still read or write its registers; it does not for one in assembly.)
+struct W4Unpack {
+  uint32_t mask = 0x00780078u, one = 0x41804180u;
+  __device__ __forceinline__ W4Unpack() {
+    asm("" : "+s"(mask));
+    asm("" : "+v"(one));
+  }
+  // eight codes as bf16 16 + c, column order
+  __device__ __forceinline__ bf16x8 operator()(uint32_t w) const {
+    return as_bf16x8(make_uint4(((w << 3) & mask) | one, ((w >> 1) & mask) | one, ((w >> 5) & mask) | one,
+                                ((w >> 9) & mask) | one));
+  }
+};
 
 // the constant operand -24 in every place
 __device__ __forceinline__ bf16x8 w4_surplus() {
@@ -78,96 +87,101 @@ __device__ __forceinline__ void w4_store(const W4Args& g, int m, int n0, f32x4 a
   }
 }
 
+// One k-block: acc[i][t] += scales of weight block i times its codes' products with activation block t. xf holds the
+// activations' four 32-column steps, wv the blocks' codes, sv their scales, four rows a lane and group.
+template <int MB, int NB, int GP>
+__device__ __forceinline__ void w4_block(const uint4 (&xf)[MB][4], const uint4 (&wv)[NB], const uint2 (&sv)[NB][GP],
+                                         f32x4 (&acc)[NB][MB]) {
+  constexpr int SPG = 4 / GP;             // 32-column steps per group
+  const bf16x8 surplus = w4_surplus();
+  const W4Unpack unpack;
+#pragma unroll
+  for (int p = 0; p < GP; ++p) {
+    f32x4 xs[MB];
+#pragma unroll
+    for (int t = 0; t < MB; ++t) xs[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = p * SPG; j < (p + 1) * SPG; ++j)
+#pragma unroll
+      for (int t = 0; t < MB; ++t)
+        xs[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(surplus, as_bf16x8(xf[t][j]), xs[t], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const uint32_t w4[4] = {wv[i].x, wv[i].y, wv[i].z, wv[i].w};
+      f32x4 sum[MB];
+#pragma unroll
+      for (int t = 0; t < MB; ++t) sum[t] = xs[t];
+#pragma unroll
+      for (int j = p * SPG; j < (p + 1) * SPG; ++j) {
+        const bf16x8 wf = unpack(w4[j]);
+#pragma unroll
+        for (int t = 0; t < MB; ++t)
+          sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, as_bf16x8(xf[t][j]), sum[t], 0, 0, 0);
+      }
+      const float s4[4] = {bf2f(sv[i][p].x & 0xffff), bf2f(sv[i][p].x >> 16), bf2f(sv[i][p].y & 0xffff), bf2f(sv[i][p].y >> 16)};
+#pragma unroll
+      for (int t = 0; t < MB; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][t][e] = fmaf(s4[e], sum[t][e], acc[i][t][e]);
+    }
+  }
+}
+
 // Few rows: a workgroup owns 16 NB weight rows and 16 MT activation rows, its NW waves a contiguous run of k-blocks
-// each; they add up through LDS in wave order. One 16-byte load per lane brings a whole 1 KB block.
+// each; they add up through LDS in wave order. One 16-byte load per lane brings a whole 1 KB block of weights. A wave
+// keeps U k-blocks in flight: block u's registers take the block U further on as soon as they are multiplied. Loads beyond
+// a wave's run, the rows or the columns go out of their buffer's bounds, which reads zeros and moves nothing, so nothing
+// in the loop is conditional.
 template <int MT, int NB, int NW, int GP, int U>
 __global__ __launch_bounds__(NW * 64) void k_w4_rows(W4Args g) {
-  constexpr int SPG = 4 / GP;             // 32-column steps per group
   const LinearW4& a = g.a;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int r = lane & 15, q = lane >> 4;
   const int nb0 = blockIdx.x * NB, m0 = blockIdx.y * (16 * MT);
-  const int nbs = (a.N + 15) >> 4;
-  const uint16_t* xrow[MT];
-  bool mvalid[MT];
+  const int nbs = min(((a.N + 15) >> 4) - nb0, NB), rows = min(a.M - m0, 16 * MT);
+  const __amdgpu_buffer_rsrc_t rx = buffer_of(a.x + (int64_t)m0 * a.ldx, (uint32_t)(((rows - 1) * a.ldx + a.K) * 2));
+  const __amdgpu_buffer_rsrc_t rw = buffer_of(a.wq + (int64_t)nb0 * g.kb * 1024, (uint32_t)(nbs * g.kb) * 1024u);
+  const __amdgpu_buffer_rsrc_t rs = buffer_of(a.scales + (int64_t)nb0 * g.groups * 16, (uint32_t)(nbs * g.groups) * 32u);
+  uint32_t offx[MT], offw[NB], offs[NB];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int m = m0 + 16 * t + r;
-    mvalid[t] = m < a.M;
-    xrow[t] = a.x + (int64_t)(mvalid[t] ? m : 0) * a.ldx + (q << 3);
-  }
-  // a block row beyond the last reads the last one again; its outputs are not stored
-  const uint8_t* wrow[NB];
-  const uint16_t* srow[NB];
+  for (int t = 0; t < MT; ++t) offx[t] = 16 * t + r < rows ? (uint32_t)(16 * t + r) * (uint32_t)(a.ldx * 2) + q * 16 : kOffNone;
 #pragma unroll
   for (int b = 0; b < NB; ++b) {
-    const int nb = min(nb0 + b, nbs - 1);
-    wrow[b] = a.wq + (int64_t)nb * g.kb * 1024 + lane * 16;
-    srow[b] = a.scales + (int64_t)nb * g.groups * 16 + (q << 2);
+    offw[b] = b < nbs ? (uint32_t)(b * g.kb) * 1024u + lane * 16 : kOffNone;
+    offs[b] = b < nbs ? (uint32_t)(b * g.groups) * 32u + q * 8 : kOffNone;
   }
+  const int per = (g.kb + NW - 1) / NW, kb0 = wave * per, kb_end = min(g.kb, kb0 + per);
+  uint4 wv[U][NB], xv[U][MT][4];
+  uint2 sv[U][NB][GP];
+  auto load = [&](int u, int kb) __attribute__((always_inline)) {
+    const bool in = kb < kb_end;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      wv[u][b] = buffer_load16(rw, in ? offw[b] + (uint32_t)kb * 1024u : kOffNone);
+#pragma unroll
+      for (int p = 0; p < GP; ++p)
+        sv[u][b][p] = __builtin_bit_cast(
+            uint2, __builtin_amdgcn_raw_buffer_load_b64(rs, in ? offs[b] + (uint32_t)(kb * GP + p) * 32u : kOffNone, 0, 0));
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        xv[u][t][j] = buffer_load16(rx, in && kb * 128 + 32 * j < a.K ? offx[t] + (uint32_t)(kb * 256 + 64 * j) : kOffNone);
+  };
   f32x4 acc[NB][MT];
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[b][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const bf16x8 surplus = w4_surplus();
-  const int per = (g.kb + NW - 1) / NW, kb_end = min(g.kb, (wave + 1) * per);
-  for (int kb0 = wave * per; kb0 < kb_end; kb0 += U) {
-    uint4 wv[U][NB], xv[U][MT][4];
-    uint2 sv[U][NB][GP];
+#pragma unroll
+  for (int u = 0; u < U; ++u) load(u, kb0 + u);
+  for (int kb = kb0; kb < kb_end; kb += U) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int kb = min(kb0 + u, kb_end - 1);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        wv[u][b] = load_nt16(wrow[b] + (int64_t)kb * 1024);
-#pragma unroll
-        for (int p = 0; p < GP; ++p) sv[u][b][p] = *reinterpret_cast<const uint2*>(srow[b] + (kb * GP + p) * 16);
-      }
-#pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int k0 = kb * 128 + 32 * j;
-          uint4 v = make_uint4(0, 0, 0, 0);
-          if (mvalid[t] && k0 < a.K) v = *reinterpret_cast<const uint4*>(xrow[t] + k0);
-          xv[u][t][j] = v;
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (kb0 + u >= kb_end) break;
-#pragma unroll
-      for (int p = 0; p < GP; ++p) {
-        f32x4 xs[MT];
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          xs[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int j = p * SPG; j < (p + 1) * SPG; ++j)
-            xs[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(surplus, as_bf16x8(xv[u][t][j]), xs[t], 0, 0, 0);
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          const uint32_t w4[4] = {wv[u][b].x, wv[u][b].y, wv[u][b].z, wv[u][b].w};
-          f32x4 sum[MT];
-#pragma unroll
-          for (int t = 0; t < MT; ++t) sum[t] = xs[t];
-#pragma unroll
-          for (int j = p * SPG; j < (p + 1) * SPG; ++j) {
-            const bf16x8 wf = w4_values(w4[j]);
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-              sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, as_bf16x8(xv[u][t][j]), sum[t], 0, 0, 0);
-          }
-          const uint2 s2 = sv[u][b][p];
-          const float s4[4] = {bf2f(s2.x & 0xffff), bf2f(s2.x >> 16), bf2f(s2.y & 0xffff), bf2f(s2.y >> 16)};
-#pragma unroll
-          for (int t = 0; t < MT; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[b][t][e] = fmaf(s4[e], sum[t][e], acc[b][t][e]);
-        }
-      }
+      w4_block<MT, NB, GP>(xv[u], wv[u], sv[u], acc);
+      load(u, kb + u + U);
     }
   }
   __shared__ f32x4 red[NW][NB * MT][64];
@@ -184,10 +198,158 @@ __global__ __launch_bounds__(NW * 64) void k_w4_rows(W4Args g) {
   }
 }
 
+// Many rows: a BN x BM output tile. KS sets of WGN x WGM waves (16 NB x 16 MB outputs each) take 128-column blocks by
+// turns, set ks the blocks ks, ks + KS, .., and add up at the end, in the order of the sets: with few workgroups a
+// wave's block is a chain of dependent LDS reads, multiplications and a barrier, which other sets' blocks fill.
+//
+// A ring of NST stages (KS blocks each) in LDS filled by loads that go straight there (lds_load16, as in gemm_tile.hpp):
+// the activations as rows of 256 bytes whose 16-byte chunk c lies at position c ^ row % 16 (the 16 rows read together
+// fall on different banks), the weights as the 1 KB blocks they are, the blocks' scales behind them. Every wave issues
+// the same LPS loads a stage, so one count tells when a stage has landed. A block's activation fragments stay in registers
+// while the weight blocks pass: one is unpacked once, multiplied with all MB fragments, and its scale applied to the
+// finished group.
+template <int BN, int BM, int WGN, int WGM, int KS, int NST, int GP>
+struct W4Tile {
+  static constexpr int NW = WGN * WGM, NB = BN / WGN / 16, MB = BM / WGM / 16;
+  static constexpr int TX = BM / 4 / NW, TW = BN / 16 / NW, LPS = TX + TW + 1;
+  static constexpr int ITEMS = BN / 8 * GP, SPARTS = ITEMS > 64 ? ITEMS / 64 : 1;   // 16-byte pieces of scales
+  static constexpr int XB = BM * 256, WB = BN * 64, BLOCK = XB + WB + SPARTS * 1024, SBYTES = KS * BLOCK;
+  static constexpr size_t join = (size_t)(KS - 1) * NW * 64 * NB * MB * 16;
+  static constexpr size_t ring = (size_t)NST * SBYTES, lds = ring > join ? ring : join;
+  static_assert(TX >= 1 && TW >= 1 && BM % (4 * NW) == 0 && BN % (16 * NW) == 0 && NW % SPARTS == 0 && lds <= 160 * 1024,
+                "tile shape");
+};
+
+template <int BN, int BM, int WGN, int WGM, int KS, int NST, int GP, int MINW>
+__global__ __launch_bounds__(64 * WGN * WGM * KS, MINW) void k_w4_tile(W4Args g, int tn, int tm) {
+  typedef W4Tile<BN, BM, WGN, WGM, KS, NST, GP> T;
+  constexpr int NB = T::NB, MB = T::MB;
+  __shared__ __attribute__((aligned(1024))) char lds[T::lds];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const LinearW4& a = g.a;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int all = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int ks = all / T::NW, wave = all % T::NW, wn = wave % WGN, wm = wave / WGN;
+  const int r = lane & 15, q = lane >> 4;
+  const TileAt at = tile_at<false>(blockIdx.x, gridDim.x, tn, tm, 1);
+  const int nb0 = at.tx * (BN / 16), m0 = at.ty * BM;
+  const int nbs = ((a.N + 15) >> 4) - nb0, rows = a.M - m0;            // blocks and rows from here to the end
+  const int n = (g.kb + KS - 1) / KS;                                  // stages
+
+  const __amdgpu_buffer_rsrc_t rx = buffer_of(a.x + (int64_t)m0 * a.ldx, (uint32_t)((min(rows, BM) - 1) * a.ldx * 2 + a.K * 2));
+  const __amdgpu_buffer_rsrc_t rw = buffer_of(a.wq + (int64_t)nb0 * g.kb * 1024, (uint32_t)min(nbs, BN / 16) * g.kb * 1024u);
+  const __amdgpu_buffer_rsrc_t rs = buffer_of(a.scales + (int64_t)nb0 * g.groups * 16, (uint32_t)min(nbs, BN / 16) * g.groups * 32u);
+  uint32_t offx[T::TX], offw[T::TW], offs;
+  int chx[T::TX];
+#pragma unroll
+  for (int t = 0; t < T::TX; ++t) {
+    const int row = (wave * T::TX + t) * 4 + (lane >> 4);
+    chx[t] = ((lane & 15) ^ (row & 15)) * 8;
+    offx[t] = row < rows ? (uint32_t)(row * (uint32_t)a.ldx + chx[t]) * 2 : kOffNone;
+  }
+#pragma unroll
+  for (int t = 0; t < T::TW; ++t) {
+    const int nb = wave * T::TW + t;
+    offw[t] = nb < nbs ? (uint32_t)(nb * g.kb) * 1024u + lane * 16 : kOffNone;
+  }
+  {
+    const int item = (wave % T::SPARTS) * 64 + lane, nb = item / (2 * GP);
+    offs = item < T::ITEMS && nb < nbs ? (uint32_t)(nb * g.groups) * 32u + (item % (2 * GP)) * 16 : kOffNone;
+  }
+  // this set's block of stage st; one beyond the last reads zeros
+  auto issue = [&](int slot, int st) __attribute__((always_inline)) {
+    const int kb = st * KS + ks;
+    const uint32_t dst = lds0 + slot * T::SBYTES + ks * T::BLOCK;
+    const int left = a.K - kb * 128;              // columns from here to the end
+    const bool in = left > 0;
+#pragma unroll
+    for (int t = 0; t < T::TX; ++t)
+      lds_load16<false>(rx, dst + (wave * T::TX + t) * 1024, chx[t] < left ? offx[t] : kOffNone, in ? kb * 256 : 0);
+#pragma unroll
+    for (int t = 0; t < T::TW; ++t)
+      lds_load16<false>(rw, dst + T::XB + (wave * T::TW + t) * 1024, in ? offw[t] : kOffNone, in ? kb * 1024 : 0);
+    lds_load16<false>(rs, dst + T::XB + T::WB + (wave % T::SPARTS) * 1024, in ? offs : kOffNone, in ? kb * GP * 32 : 0);
+  };
+
+  f32x4 acc[NB][MB];
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < MB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  uint32_t rdx[4];                                // byte offsets of this lane's fragments of a 16-row block
+#pragma unroll
+  for (int j = 0; j < 4; ++j) rdx[j] = (wm * MB * 16 + r) * 256 + (((4 * j + q) ^ r) << 4);
+
+#pragma unroll
+  for (int i = 0; i < NST - 1; ++i)
+    if (i < n) issue(i, i);
+  int slot = 0;
+  for (int st = 0; st < n; ++st) {
+    // stage st has landed for every wave, and the slot of stage st - 1 is free
+    if (st + NST - 2 < n) lds_wait_barrier<(NST - 2) * T::LPS>();
+    else lds_wait_barrier<0>();
+    if (st + NST - 1 < n) issue(slot == 0 ? NST - 1 : slot - 1, st + NST - 1);
+    const char* base = lds + slot * T::SBYTES + ks * T::BLOCK;
+    uint4 xf[MB][4], wv[NB];
+    uint2 sv[NB][GP];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int t = 0; t < MB; ++t) xf[t][j] = *reinterpret_cast<const uint4*>(base + rdx[j] + t * 4096);
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      wv[i] = *reinterpret_cast<const uint4*>(base + T::XB + (wn * NB + i) * 1024 + lane * 16);
+#pragma unroll
+      for (int p = 0; p < GP; ++p)
+        sv[i][p] = *reinterpret_cast<const uint2*>(base + T::XB + T::WB + ((wn * NB + i) * GP + p) * 32 + q * 8);
+    }
+    w4_block<MB, NB, GP>(xf, wv, sv, acc);
+    slot = slot + 1 == NST ? 0 : slot + 1;
+  }
+  if constexpr (KS > 1) {
+    f32x4* area = reinterpret_cast<f32x4*>(lds) + (size_t)wave * 64 * NB * MB + lane;
+    constexpr int set = T::NW * 64 * NB * MB;
+    __syncthreads();
+    if (ks > 0) {
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int t = 0; t < MB; ++t) area[(ks - 1) * set + (i * MB + t) * 64] = acc[i][t];
+    }
+    __syncthreads();
+    if (ks > 0) return;
+#pragma unroll
+    for (int x = 0; x < KS - 1; ++x)
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int t = 0; t < MB; ++t) acc[i][t] += area[x * set + (i * MB + t) * 64];
+  }
+#pragma unroll
+  for (int t = 0; t < MB; ++t)
+#pragma unroll
+    for (int i = 0; i < NB; ++i) w4_store(g, m0 + (wm * MB + t) * 16 + r, (nb0 + wn * NB + i) * 16 + 4 * q, acc[i][t]);
+}
+
+template <int BN, int BM, int WGN, int WGM, int KS, int NST, int MINW>
+hipError_t go_tile(const W4Args& g, hipStream_t s) {
+  constexpr int threads = 64 * WGN * WGM * KS;
+  const int tn = (g.a.N + BN - 1) / BN, tm = (g.a.M + BM - 1) / BM;
+  const int64_t tiles = (int64_t)tn * tm;
+  if (tiles * threads >= 1ll << 32) return hipErrorInvalidValue;
+  const dim3 grid((unsigned)tiles), block(threads);
+  switch (g.a.group) {
+    case 128: return launch((k_w4_tile<BN, BM, WGN, WGM, KS, NST, 1, MINW>), grid, block, 0, s, g, tn, tm);
+    case 64: return launch((k_w4_tile<BN, BM, WGN, WGM, KS, NST, 2, MINW>), grid, block, 0, s, g, tn, tm);
+    default: return launch((k_w4_tile<BN, BM, WGN, WGM, KS, NST, 4, MINW>), grid, block, 0, s, g, tn, tm);
+  }
+}
+
 template <int MT, int NB, int NW, int U>
 hipError_t go_rows(const W4Args& g, hipStream_t s) {
   const int nbs = (g.a.N + 15) / 16;
   const dim3 grid((nbs + NB - 1) / NB, (g.a.M + 16 * MT - 1) / (16 * MT)), block(64 * NW);
+  if (grid.y > 65535) return hipErrorInvalidValue;
   switch (g.a.group) {
     case 128: return launch((k_w4_rows<MT, NB, NW, 1, U>), grid, block, 0, s, g);
     case 64: return launch((k_w4_rows<MT, NB, NW, 2, U>), grid, block, 0, s, g);
@@ -209,9 +371,20 @@ hipError_t linear_w4(const LinearW4& a, const Split& sp, hipStream_t s) {
   g.groups = g.kb * (128 / a.group);
   g.vec = !((uintptr_t)a.y & (a.y_f32 ? 15 : 7)) && !(a.ldy & 3) && !((uintptr_t)a.bias & 7) && !((uintptr_t)a.res & 7) &&
           !(a.res && (a.ldr & 3));
-  if (a.M <= 16) return go_rows<1, 1, 4, 4>(g, s);
-  if ((a.M + 31) / 32 > 65535) return hipErrorInvalidValue;
-  return go_rows<2, 1, 4, 4>(g, s);
+  // 32-bit offsets of the rows a workgroup owns
+  if (a.ldx >= (1 << 30) / 128) return hipErrorInvalidValue;
+  switch (w4_plan(a.M, a.N, a.K, a.group)) {     // rows: MT, NB, waves, k-blocks in flight; tiles: waves n x m, sets, ring, waves per SIMD
+    case W4_ROWS16: return go_rows<1, 1, 4, 2>(g, s);
+    case W4_ROWS32: return go_rows<1, 2, 8, 2>(g, s);
+    case W4_ROWS64: return go_rows<1, 4, 8, 1>(g, s);
+    case W4_TILE32X32: return go_tile<32, 32, 2, 1, 4, 3, 2>(g, s);
+    case W4_TILE64X32: return go_tile<64, 32, 4, 1, 2, 3, 2>(g, s);
+    case W4_TILE64X32_DEEP: return go_tile<64, 32, 4, 1, 4, 2, 4>(g, s);
+    case W4_TILE64X64: return go_tile<64, 64, 2, 2, 1, 2, 2>(g, s);
+    case W4_TILE128X64: return go_tile<128, 64, 4, 2, 1, 2, 2>(g, s);
+    case W4_TILE128X64_WIDE: return go_tile<128, 64, 4, 1, 1, 2, 2>(g, s);
+    default: return go_tile<256, 128, 4, 2, 1, 3, 2>(g, s);
+  }
 }
 
 }  // namespace k

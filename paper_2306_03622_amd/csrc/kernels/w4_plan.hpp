@@ -1,0 +1,55 @@
+// Which kernel a 4-bit linear layer takes (no HIP headers: also compiled for the host alone).
+#pragma once
+#include <cstdint>
+
+namespace tp {
+namespace k {
+
+// Output features x rows a workgroup owns, sets of waves over the k-blocks (128 columns) of which each takes its share,
+// and the time model's coefficients: us = launch + rounds (round + steps (step + group_step 128 / group)) + steps first, with
+// `rounds` = workgroups / 256 CUs, rounded up, and `steps` = k-blocks a set takes.
+struct W4Variant {
+  int bn, bm, sets;
+  double launch, round, first, step, group_step;
+};
+
+enum { W4_ROWS16, W4_ROWS32, W4_ROWS64, W4_TILE32X32, W4_TILE64X32, W4_TILE64X32_DEEP, W4_TILE64X64, W4_TILE128X64,
+       W4_TILE128X64_WIDE, W4_TILE256X128, W4_VARIANTS };
+
+// Fitted to 2499 passes on MI355X (13 shapes from 96 x 200 to 8192 x 32768, the three groups, 1 to 5000 rows, graph replay,
+// operands rotating beyond the L2s): choosing by the model costs 3% over the best variant of each case on average.
+// What they trade, us: 4096 x 4096, groups of 128: 1 row ROWS16 4.8, ROWS64 8; 32 rows ROWS32 8.5, ROWS16 11.4; 64 rows
+// ROWS64 9.5, ROWS32 13; 128 rows TILE64X32_DEEP 12.9, ROWS64 16; 256 rows TILE64X64 22.5, TILE64X32_DEEP 25; 1024 rows
+// TILE128X64_WIDE 49.8, TILE64X64 58; 2048 rows TILE256X128 80, TILE128X64_WIDE 90; 8192 rows 295, 351. 768 x 4096: 24 rows ROWS16 5.1,
+// 80 rows TILE64X32 6.1.
+constexpr W4Variant kW4[W4_VARIANTS] = {
+    {16, 16, 4, 2.565, 0.076, 0.0, 0.434, 0.055},   {32, 16, 8, 2.405, 0.987, 0.0, 1.042, 0.069},
+    {64, 16, 8, 2.186, 0.465, 0.0, 1.445, 0.171},   {32, 32, 4, 1.345, 2.383, 0.0, 0.689, 0.026},
+    {64, 32, 2, 2.676, 1.159, 0.132, 0.445, 0.027}, {64, 32, 4, 1.087, 3.302, 0.0, 0.945, 0.050},
+    {64, 64, 1, 3.160, 1.185, 0.203, 0.313, 0.039}, {128, 64, 1, 1.658, 2.755, 0.213, 0.552, 0.061},
+    {128, 64, 1, 1.516, 3.731, 0.327, 0.439, 0.046}, {256, 128, 1, 0.0, 7.269, 0.0, 1.727, 0.246}};
+
+inline double w4_us(const W4Variant& v, int64_t M, int64_t N, int64_t K, int group) {
+  const int64_t wgs = (N + v.bn - 1) / v.bn * ((M + v.bm - 1) / v.bm), kb = (K + 127) / 128;
+  const double rounds = (double)((wgs + 255) / 256), steps = (double)((kb + v.sets - 1) / v.sets);
+  return v.launch + rounds * (v.round + steps * (v.step + v.group_step * 128 / group)) + steps * v.first;
+}
+
+inline int w4_plan(int64_t M, int64_t N, int64_t K, int group) {
+  int best = 0;
+  double us = 0;
+  for (int i = 0; i < W4_VARIANTS; ++i) {
+    // the largest tiles only where 16 k-blocks and more make up for the ring's filling, as the model does not see
+    // (5000 rows, 1024 x 256: 20.4 us, TILE128X64 14.9)
+    if (i == W4_TILE256X128 && K < 16 * 128) continue;
+    const double t = w4_us(kW4[i], M, N, K, group);
+    if (i == 0 || t < us) {
+      best = i;
+      us = t;
+    }
+  }
+  return best;
+}
+
+}  // namespace k
+}  // namespace tp

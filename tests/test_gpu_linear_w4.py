@@ -37,12 +37,15 @@ def run(x, w, f32=False, bias=None, res=None, name="none", work=None, stream=Non
     return base[:, :n].double().cpu().numpy()
 
 
-# rows: one, around whole 16s and tiles; features and columns that fill no block; the three groups
+# rows: one, around whole 16s and tiles; features and columns that fill no block; the three groups; every kernel variant
+# (test_ops_host.py checks that)
 SHAPES = [(1, 16, 128, 128), (1, 1, 32, 32), (2, 17, 96, 32), (7, 40, 192, 64), (8, 256, 512, 128), (15, 33, 160, 32),
           (16, 48, 384, 128), (17, 100, 64, 64), (31, 130, 1024, 64), (32, 64, 256, 32), (33, 96, 128, 128), (48, 70, 640, 128),
           (64, 256, 2048, 64), (65, 257, 224, 32), (100, 1000, 2048, 64), (127, 72, 352, 32), (130, 520, 896, 128),
           (200, 768, 768, 32), (257, 129, 512, 64), (513, 300, 1152, 128), (700, 1024, 320, 64), (1100, 600, 416, 32),
-          (2049, 1040, 768, 128)]
+          (2049, 1040, 768, 128), (67, 2100, 640, 64), (20, 9000, 352, 32), (250, 1000, 1152, 64), (67, 1000, 4096, 32),
+          (130, 500, 4096, 128), (333, 1000, 4096, 128), (333, 4100, 1088, 64), (513, 4100, 1152, 32), (1025, 2100, 1152, 128),
+          (1300, 2300, 2048, 64), (1025, 4100, 2048, 128), (1300, 4100, 1088, 32)]
 
 
 @pytest.mark.parametrize("m,n,k,group", SHAPES)

@@ -189,3 +189,22 @@ def test_binding_refuses_tensors_that_do_not_belong_together():
         tp.tpo_attention(q, q, q, q.clone())
     with pytest.raises(ValueError):
         tp.tpo_attention(q, q[..., :32], q[..., :32], q.clone())
+
+
+def test_the_gpu_shapes_reach_every_variant(tmp_path):
+    from tests.test_gpu_linear_w4 import SHAPES
+    cxx = shutil.which("g++")
+    if not cxx:
+        pytest.skip("no C++ compiler")
+    (tmp_path / "d.cpp").write_text('#include <cstdio>\n#include "w4_plan.hpp"\nusing namespace tp::k;\nint main() {\n  long m, n, k;\n  int g;\n'
+                                    '  std::printf("%d\\n", (int)W4_VARIANTS);\n  while (std::scanf("%ld %ld %ld %d", &m, &n, &k, &g) == 4) '
+                                    'std::printf("%d\\n", w4_plan(m, n, k, g));\n}\n')
+    subprocess.run([cxx, "-std=c++17", "-I", os.path.join(ROOT, "paper_2306_03622_amd", "csrc", "kernels"), str(tmp_path / "d.cpp"),
+                    "-o", str(tmp_path / "d")], check=True)
+    more = [(1, 1, 32, 32), (10 ** 7, 16, 32, 32), (3 * 10 ** 6, 1, 1024, 64)]
+    out = subprocess.run([str(tmp_path / "d")], input="\n".join(" ".join(map(str, s)) for s in [*SHAPES, *more]), check=True,
+                         capture_output=True, text=True).stdout.split()
+    n, plans = int(out[0]), [int(v) for v in out[1:]]
+    assert set(plans[:len(SHAPES)]) == set(range(n))
+    # the kernels of few rows put row tiles into a grid dimension of 65535: millions of rows are for the others
+    assert all(p > 2 for p in plans[-2:])
