@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -564,20 +565,33 @@ def tpo_w4_quantize(w: np.ndarray, group: int, L=None):
     return codes, scales
 
 
-def _same_device(device, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError(f"{name} is on {t.device}, not on {device}")
+# A call's argument block is packed at once (struct, native layout) and handed over as bytes: setting the fields of a ctypes
+# structure one by one took 1.5 us of a 6 us call.
+_LINEAR = struct.Struct("@PqPPPPqPqiiiiiiPQ")
+_ATTENTION = struct.Struct("@PPPP12qPP10ifPQ")
+_ops = None
 
 
-def _launch_on(device, stream):
-    """The raw stream of a call on `device`: the caller's, which must belong to it, or the device's current one."""
-    import torch
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(device.index)
+def _op_calls():
+    """(torch, its raw current stream by device, tpo_linear_w4, tpo_attention), the last two on packed arguments."""
+    global _ops
+    if _ops is None:
+        import torch
+        L = lib()
+        calls = []
+        for name in ("tpo_linear_w4", "tpo_attention"):
+            f = L[name]                   # a function object of its own
+            f.argtypes, f.restype = [C.c_char_p, _P], C.c_int32
+            calls.append(f)
+        _ops = (torch, torch._C._cuda_getCurrentRawStream, *calls)
+    return _ops
+
+
+def _stream_of(device, stream):
+    """The raw stream of the caller's, which must belong to the tensors' device."""
     owner = getattr(stream, "device", None)
-    if owner is not None and owner != device:
-        raise ValueError(f"stream of {owner}, tensors on {device}")
+    if owner is not None and owner.index != device:
+        raise ValueError(f"stream of {owner}, tensors on device {device}")
     return _ptr(stream)
 
 
@@ -593,10 +607,10 @@ class W4Weight:
             raise ValueError(f"{codes.numel()} code bytes and {2 * scales.numel()} scale bytes, need {cb} and {sb}")
         if not (codes.is_contiguous() and scales.is_contiguous()):
             raise ValueError("codes and scales must be contiguous")
-        if codes.device.type != "cuda":
-            raise ValueError(f"codes on {codes.device}")
-        _same_device(codes.device, scales=scales)
+        if codes.device.type != "cuda" or scales.device != codes.device:
+            raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
         self.codes, self.scales, self.device = codes, scales, codes.device
+        self._packed = (codes.device.index, codes.data_ptr(), scales.data_ptr())
         self.out_features, self.in_features, self.group = out_features, in_features, group
 
     @classmethod
@@ -608,43 +622,62 @@ class W4Weight:
                    codes.shape[0], 2 * codes.shape[1], group)
 
 
-def _rows(t, name, rows, cols, dtypes):
-    """Address and row stride of a [rows][cols] tensor whose rows are contiguous."""
+def _check_rows(name, t, rows, cols, dtypes, device):
+    """Raises for a tensor that is not a [rows][cols] one with contiguous rows, of these types, on this device."""
     if t.dtype not in dtypes:
         raise ValueError(f"{name} is {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if tuple(t.shape) != (rows, cols):
         raise ValueError(f"{name} is {tuple(t.shape)}, need {(rows, cols)}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, the weight on device {device}")
     if cols > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}: rows must be contiguous")
-    return t.data_ptr(), t.stride(0) if rows > 1 else cols + -cols % 8
 
 
 def tpo_linear_w4(x, weight: W4Weight, out, bias=None, res=None, act: str = "none", work=None, stream=None):
     """out = act(x W^T + bias + res): x, res bf16 [M][K] and [M][N], out bf16 or fp32 [M][N], bias bf16 [N], all on the
     weight's device. stream: a torch stream of that device (default: its current one); work: a uint8 tensor of scratch."""
-    import torch
+    torch, current, call, _ = _ops or _op_calls()
     bf = torch.bfloat16
+    dev, codes, scales = weight._packed
     n, k = weight.out_features, weight.in_features
-    _same_device(weight.device, x=x, out=out, bias=bias, res=res, work=work)
-    a = tpo_linear_w4_args()
     m = x.shape[0]
-    a.x, a.ldx = _rows(x, "x", m, k, (bf,))
-    a.y, a.ldy = _rows(out, "out", m, n, (bf, torch.float32))
-    a.y_dtype = TP_BF16 if out.dtype == bf else TP_F32
-    a.wq, a.scales = weight.codes.data_ptr(), weight.scales.data_ptr()
+    f32 = out.dtype is torch.float32
+    if (x.dtype is not bf or x.shape != (m, k) or x.get_device() != dev or x.stride(1) != 1 or out.shape != (m, n) or
+            not (f32 or out.dtype is bf) or out.get_device() != dev or (n > 1 and out.stride(1) != 1)):
+        _check_rows("x", x, m, k, (bf,), dev)
+        _check_rows("out", out, m, n, (bf, torch.float32), dev)
+    ldx, ldy = (x.stride(0), out.stride(0)) if m > 1 else (k, n)
+    bp = rp = ldr = wp = wb = 0
     if bias is not None:
-        if bias.dtype != bf or bias.shape != (n,) or not bias.is_contiguous():
-            raise ValueError(f"bias must be a contiguous bfloat16 [{n}]")
-        a.bias = bias.data_ptr()
+        if bias.dtype is not bf or bias.shape != (n,) or not bias.is_contiguous() or bias.get_device() != dev:
+            raise ValueError(f"bias must be a contiguous bfloat16 [{n}] on device {dev}")
+        bp = bias.data_ptr()
     if res is not None:
-        a.res, a.ldr = _rows(res, "res", m, n, (bf,))
-    a.M, a.N, a.K, a.group, a.act = m, n, k, weight.group, TP_ACT[act]
+        _check_rows("res", res, m, n, (bf,), dev)
+        rp, ldr = res.data_ptr(), res.stride(0) if m > 1 else n
     if work is not None:
-        a.work, a.work_bytes = work.data_ptr(), work.numel() * work.element_size()
-    L = _lib or lib()
-    status = L.tpo_linear_w4(a, _launch_on(weight.device, stream))
+        if work.get_device() != dev:
+            raise ValueError(f"work is on {work.device}, the weight on device {dev}")
+        wp, wb = work.data_ptr(), work.numel() * work.element_size()
+    status = call(_LINEAR.pack(x.data_ptr(), ldx, codes, scales, bp, rp, ldr, out.data_ptr(), ldy, TP_F32 if f32 else TP_BF16,
+                               m, n, k, weight.group, TP_ACT[act], wp, wb),
+                  current(dev) if stream is None else _stream_of(dev, stream))
     if status != TP_OK:
-        _check(L, status)
+        _check(lib(), status)
+
+
+def _strides(name, t, bf, dev):
+    """A [B][tokens][heads][dim] tensor's first three strides, 0 for a dimension of one entry, which is never stepped."""
+    if t.dtype is not bf:
+        raise ValueError(f"{name} is {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, q on device {dev}")
+    s0, s1, s2, s3 = t.stride()
+    if s3 != 1:
+        raise ValueError(f"{name}: the values of a head must be contiguous")
+    n0, n1, n2, _ = t.shape
+    return s0 if n0 > 1 else 0, s1 if n1 > 1 else 0, s2 if n2 > 1 else 0
 
 
 def tpo_attention(q, k, v, out, q_lens=None, kv_lens=None, causal: bool = False, window=(-1, -1), sinks: int = 0,
@@ -652,41 +685,35 @@ def tpo_attention(q, k, v, out, q_lens=None, kv_lens=None, causal: bool = False,
     """Attention of q [B][q_len][heads][dim] over k, v [B][kv_len][kv_heads][dim] into out (as q), bf16, with any strides
     but the last. q_lens, kv_lens: int32 [B] on the device; window: keys to the left and right of a query's
     position that it sees (negative: all); sinks: first keys that it sees besides; see torpor_ops.h."""
-    import torch
     if q.dim() != 4 or k.dim() != 4 or v.shape != k.shape or out.shape != q.shape:
         raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}, out {tuple(out.shape)}")
     b, nq, h, d = q.shape
-    if k.shape[0] != b or k.shape[3] != d:
+    kb, nk, hk, kd = k.shape
+    if kb != b or kd != d:
         raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)}")
-    dev = q.device
-    if dev.type != "cuda":
-        raise ValueError(f"q on {dev}")
-    _same_device(dev, k=k, v=v, out=out, q_lens=q_lens, kv_lens=kv_lens, work=work)
-    a = tpo_attention_args()
-    for name, t, st in (("q", q, a.q_stride), ("k", k, a.k_stride), ("v", v, a.v_stride), ("out", out, a.out_stride)):
-        if t.dtype != torch.bfloat16:
-            raise ValueError(f"{name} is {t.dtype}")
-        s0, s1, s2, s3 = t.stride()
-        if s3 != 1:
-            raise ValueError(f"{name}: the values of a head must be contiguous")
-        # the stride of a dimension of one entry is never used
-        n0, n1, n2, _ = t.shape
-        st[0], st[1], st[2] = s0 if n0 > 1 else 0, s1 if n1 > 1 else 0, s2 if n2 > 1 else 0
-    for name, t in (("q_lens", q_lens), ("kv_lens", kv_lens)):
-        if t is not None and (t.dtype != torch.int32 or t.shape != (b,) or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous int32 [{b}]")
-    a.q, a.k, a.v, a.out = q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr()
-    a.q_lens = None if q_lens is None else q_lens.data_ptr()
-    a.kv_lens = None if kv_lens is None else kv_lens.data_ptr()
-    a.batch, a.heads, a.kv_heads, a.head_dim, a.q_len, a.kv_len = b, h, k.shape[2], d, nq, k.shape[1]
-    a.causal, a.sinks, a.scale = int(causal), sinks, scale
-    a.window_left, a.window_right = window
+    dev = q.get_device()
+    if dev < 0:
+        raise ValueError(f"q on {q.device}")
+    torch, current, _, call = _ops or _op_calls()
+    bf = torch.bfloat16
+    lens = [0, 0]
+    for i, t in enumerate((q_lens, kv_lens)):
+        if t is not None:
+            if t.dtype is not torch.int32 or t.shape != (b,) or not t.is_contiguous() or t.get_device() != dev:
+                raise ValueError(f"{('q_lens', 'kv_lens')[i]} must be a contiguous int32 [{b}] on device {dev}")
+            lens[i] = t.data_ptr()
+    wp = wb = 0
     if work is not None:
-        a.work, a.work_bytes = work.data_ptr(), work.numel() * work.element_size()
-    L = _lib or lib()
-    status = L.tpo_attention(a, _launch_on(dev, stream))
+        if work.get_device() != dev:
+            raise ValueError(f"work is on {work.device}, q on device {dev}")
+        wp, wb = work.data_ptr(), work.numel() * work.element_size()
+    left, right = window
+    status = call(_ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), *_strides("q", q, bf, dev),
+                                  *_strides("k", k, bf, dev), *_strides("v", v, bf, dev), *_strides("out", out, bf, dev), *lens,
+                                  b, h, hk, d, nq, nk, causal, left, right, sinks, scale, wp, wb),
+                  current(dev) if stream is None else _stream_of(dev, stream))
     if status != TP_OK:
-        _check(L, status)
+        _check(lib(), status)
 
 
 _probe = None

@@ -45,6 +45,17 @@ def test_ctypes_layout_matches_the_header(name, tmp_path):
     assert {f: int(v) for f, v in got.items()} == {f: getattr(cls, f).offset for f, _ in cls._fields_}
 
 
+def test_packed_arguments_have_the_structs_layout():
+    for packer, cls, values in ((T._LINEAR, T.tpo_linear_w4_args, list(range(1, 18))),
+                                (T._ATTENTION, T.tpo_attention_args, [*range(1, 29), 0.5, 30, 31])):
+        assert packer.size == ctypes.sizeof(cls)
+        a, got = cls.from_buffer_copy(packer.pack(*values)), []
+        for name, _ in cls._fields_:
+            v = getattr(a, name)
+            got += list(v) if hasattr(v, "__len__") else [v]
+        assert got == values
+
+
 def unblock(codes, scales, n, k, group):
     """The matrix of blocked codes and scales, element by element from the format's description."""
     kb, ng = (k + 127) // 128, (k + 127) // 128 * (128 // group)
