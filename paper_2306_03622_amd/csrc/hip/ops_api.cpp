@@ -114,6 +114,7 @@ tp_status tpo_attention(const tpo_attention_args* a, void* stream) {
   for (const int64_t* st : {a->q_stride, a->k_stride, a->v_stride, a->out_stride})
     for (int i = 0; i < 3; ++i)
       if (st[i] < 0 || st[i] % 8 || st[i] > kMostStride) return inval(who, "strides must be multiples of 8, not negative, below 2^40");
+  if (a->k_stride[1] > 1 << 23 || a->v_stride[1] > 1 << 23) return inval(who, "token strides of k and v must be at most 2^23");
   {
     // rows of the output must not share memory
     const int64_t n[3] = {a->batch, a->q_len, a->heads};

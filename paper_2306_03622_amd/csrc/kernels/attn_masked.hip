@@ -4,23 +4,26 @@
 // The query heads that share a key/value head are handled together: row rho of a sequence is head rho % G of the group at
 // query rho / G (G heads per key/value head), so keys and values are read once for all of them. A workgroup
 // takes 32 WR rows (WR waves of 32 side by side, each set WK waves deep over the keys) and walks tiles of 32 KPW WK
-// keys, which it stages row-major in LDS; the next tile's loads are in flight meanwhile.
+// keys through a ring of NST stages in LDS, filled by loads that go straight there (lds_load16, as in gemm_tile.hpp): rows
+// as they lie in memory, the 16-byte chunk c of a row at position c ^ row, so that the rows read together fall on
+// different banks. One barrier per tile; keys beyond the sequence are out of the buffer's bounds and read as zeros.
 //
 // Scores are computed transposed, S^T = K Q^T: lane l holds row l % 32 against keys 8 (i / 4) + 4 (l / 32) + i % 4 in
 // register i, so a row's maximum and sum stay in a lane and its partner l ^ 32. The output is transposed too, O^T =
 // V^T P^T: the exponentials, rounded to bf16 (as the matrix cores take them; the sum that divides
 // them is of the unrounded ones), are the B operand from the very registers they are in, V^T is read with the transposing
-// LDS load, and a row's rescaling is one factor per lane.
+// LDS load, and a row's rescaling is one factor per lane. The reference that exponents are taken from follows the maximum only
+// when that has risen by 8 (a factor of 256, harmless in fp32 sums and in bf16, whose precision is relative).
 //
 // A key is seen if it lies in [lo, hi] (window and order) or in front of sk (sinks), three numbers per row. Only
-// tiles that hold a seen key are walked, and only those not seen whole by every row are masked. There a score is replaced, not
-// added to, so a hidden key may hold anything; its value row, which 0 would multiply, may hold infinities or NaN: staging
-// replaces those by 0 in masked tiles, and a tile that had any is followed by a second pass that counts, for each
-// row and column, the replaced values of seen keys and sets the output accordingly.
+// tiles that hold a key seen by some row are walked, a wave passes over those that its own rows do not see, and only those
+// that they do not see whole are masked. There a score is replaced, not added to, so a hidden key may hold anything. Its value
+// row, which 0 would multiply, may hold infinities or NaN: those show as NaN in the sums, and a workgroup that finds
+// any such result at the end walks its keys twice more: once with what is not finite replaced by 0, and once counting,
+// for each row and column, the replaced values of seen keys, which then set the output.
 #include <algorithm>
 
-#include "common.hpp"
-#include "kernels.hpp"
+#include "gemm_tile.hpp"
 
 namespace tp {
 namespace k {
@@ -70,10 +73,7 @@ struct Walk {
   __device__ __forceinline__ int tile(int t) const { return t < ns ? t : w0 + t - ns; }
 };
 
-// bit pattern of a bf16 infinity or NaN in the low or high half
-__device__ __forceinline__ bool odd_half(uint32_t w) {
-  return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u;
-}
+// two bf16 with infinities and NaN as 0
 __device__ __forceinline__ uint32_t zero_odd(uint32_t w) {
   if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
   if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
@@ -86,29 +86,39 @@ __device__ __forceinline__ uint32_t odd_code(uint32_t h) {
 }
 __device__ __forceinline__ uint32_t odd_codes(uint32_t w) { return odd_code(w & 0xffff) | odd_code(w >> 16) << 16; }
 
-template <int D, int WR, int WK, int KPW>
-__global__ __launch_bounds__(64 * WR * WK) void k_attention_masked(AttnArgs g) {
-  constexpr int NT = 64 * WR * WK, KT = 32 * KPW * WK;
-  constexpr int LDK = D + 8, LDV = D + 16;          // row strides in LDS: reads of 16 rows fall on different banks
-  constexpr int CH = D / 8, NL = KT * CH / NT;      // 16-byte pieces of a key, loads per thread and tile
-  constexpr int DT = D / 32;
-  static_assert(KT * CH % NT == 0, "whole loads");
-  constexpr int KV = (LDK + LDV) * KT * 2, MERGE = WK > 1 ? (WK - 1) * WR * 64 * (DT * 16 + 2) * 4 : 0;
-  __shared__ __attribute__((aligned(16))) char lds[KV > MERGE ? KV : MERGE];
-  __shared__ int odd[2];                            // of the tiles by turns, see the loop
-  uint16_t* Ks = reinterpret_cast<uint16_t*>(lds);
-  uint16_t* Vs = Ks + LDK * KT;
+// FAST: the hot loop. CLEAN: the same with V's infinities and NaN as zeros. COUNT: those that are seen, as sums of their kinds.
+enum { FAST, CLEAN, COUNT };
+
+template <int D, int WR, int WK, int KPW, int NST>
+struct AttnTile {
+  static constexpr int NW = WR * WK, KT = 32 * KPW * WK;
+  static constexpr int ROW = 2 * D, CPR = ROW / 16, RPL = 1024 / ROW;          // bytes and chunks of a row, rows a load
+  static constexpr int LOADS = KT / RPL / NW, LPS = 2 * LOADS;                 // of K (and of V), in all, per wave
+  static constexpr int KB = KT * ROW, SBYTES = 2 * KB, DT = D / 32;
+  static constexpr int REC = DT * 16 + 2;                                      // a lane's results when waves join
+  static constexpr int join = (WK - 1) * WR * 64 * REC * 4, lds = NST * SBYTES > join ? NST * SBYTES : join;
+  static_assert(KT % (RPL * NW) == 0 && LOADS >= 1 && KPW <= 2 && NST >= 2 && lds <= 160 * 1024, "tile shape");
+};
+
+template <int D, int WR, int WK, int KPW, int NST, int MINW>
+__global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArgs g) {
+  typedef AttnTile<D, WR, WK, KPW, NST> T;
+  constexpr int KT = T::KT, DT = T::DT;
+  __shared__ __attribute__((aligned(1024))) char lds[T::lds];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
 
   const Attention& a = g.a;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % WR, wk = wave / WR;
   const int c = lane & 31, h = lane >> 5;
+  // key/value heads first, so that workgroups handed out together read different ones and an XCD the same ones again;
+  // the last rows, which see the most keys under a causal order, before the others
   int id = blockIdx.x;
-  const int z = id % g.splits;
-  id /= g.splits;
-  const int rt = id % g.tiles;
-  id /= g.tiles;
-  const int hk = id % a.kv_heads, b = id / a.kv_heads;
+  const int bh = id % (a.kv_heads * a.batch);
+  id /= a.kv_heads * a.batch;
+  const int z = id % g.splits, rt = g.tiles - 1 - id / g.splits;
+  const int hk = bh % a.kv_heads, b = bh / a.kv_heads;
 
   int qn = a.q_lens ? a.q_lens[b] : a.q_len, kn = a.kv_lens ? a.kv_lens[b] : a.kv_len;
   qn = min(max(qn, 0), a.q_len);
@@ -132,10 +142,14 @@ __global__ __launch_bounds__(64 * WR * WK) void k_attention_masked(AttnArgs g) {
   const int n = w.count();
   const int t0 = (int)((int64_t)n * z / g.splits), t1 = (int)((int64_t)n * (z + 1) / g.splits);
 
-  // this lane's row of Q (the last one again where there is none) and what it sees
+  // this lane's row of Q (the last one again where there is none) and what it sees; what the wave's rows see
   const bool live = row < rows;
   const int li = live ? qi : qn - 1, lh = live ? qh : hk * g.share + g.share - 1;
   const Seen me = seen_at(a, li + shift, kn);
+  const int wrow = row0 + wr * 32;
+  const bool idle = wrow >= rows;
+  const Seen v0 = seen_at(a, wrow / g.share + shift, kn);
+  const Seen v1 = seen_at(a, (min(wrow + 32, rows) - 1) / g.share + shift, kn);
   const uint16_t* qrow = a.q + (int64_t)b * a.qs[0] + (int64_t)li * a.qs[1] + (int64_t)lh * a.qs[2] + 8 * h;
   uint4 qf[D / 16];
 #pragma unroll
@@ -143,94 +157,75 @@ __global__ __launch_bounds__(64 * WR * WK) void k_attention_masked(AttnArgs g) {
 
   const uint16_t* kbase = a.k + (int64_t)b * a.ks[0] + (int64_t)hk * a.ks[2];
   const uint16_t* vbase = a.v + (int64_t)b * a.vs[0] + (int64_t)hk * a.vs[2];
-  uint4 kr[NL], vr[NL];
-  // keys beyond the sequence are not read and count as zero
-  auto load = [&](int tile) __attribute__((always_inline)) {
+  // load i of this wave: rows lrow + i RPL of a tile, at the chunk that belongs at the lane's position
+  const int lrow = wave * T::LOADS * T::RPL + lane / T::CPR;
+  auto issue = [&](int slot, int tile) __attribute__((always_inline)) {
+    const __amdgpu_buffer_rsrc_t rk = buffer_of(kbase + (int64_t)tile * KT * a.ks[1], 0x7fffffffu);
+    const __amdgpu_buffer_rsrc_t rv = buffer_of(vbase + (int64_t)tile * KT * a.vs[1], 0x7fffffffu);
+    const uint32_t dst = lds0 + slot * T::SBYTES + wave * T::LOADS * 1024;
+    const int left = kn - tile * KT;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int at = i * NT + tid, key = tile * KT + at / CH, d = (at % CH) * 8;
-      kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
-      if (key < kn) {
-        kr[i] = *reinterpret_cast<const uint4*>(kbase + (int64_t)key * a.ks[1] + d);
-        vr[i] = *reinterpret_cast<const uint4*>(vbase + (int64_t)key * a.vs[1] + d);
-      }
+    for (int i = 0; i < T::LOADS; ++i) {
+      const int r = lrow + i * T::RPL;
+      const uint32_t ch = (uint32_t)((lane % T::CPR) ^ (r % T::CPR)) * 16;
+      lds_load16<false>(rk, dst + i * 1024, r < left ? (uint32_t)r * (uint32_t)(a.ks[1] * 2) + ch : kOffNone, 0);
+      lds_load16<false>(rv, dst + T::KB + i * 1024, r < left ? (uint32_t)r * (uint32_t)(a.vs[1] * 2) + ch : kOffNone, 0);
     }
   };
 
   f32x16 o[DT];
-#pragma unroll
-  for (int t = 0; t < DT; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-  float top = -INFINITY, total = 0.f;               // maximum (in base-2 exponents), this lane's half of the sum
+  float top, total;                                 // reference of the exponents (base 2), this lane's half of the sum
   const float c2 = a.scale * 1.44269504088896341f;
 
-  // V^T P^T for this wave's keys of the tile in LDS
-  const uint16_t* vread = Vs + (wk * KPW * 32 + 4 * h + ((lane & 15) >> 2)) * LDV + 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
-  auto values = [&](const uint4 (&pb)[2 * KPW], f32x16 (&out)[DT]) __attribute__((always_inline)) {
+  // byte addresses of this lane's fragments inside a stage, for the wave's first 32 keys: K rows, chunk 2 i + h; V^T pieces
+  // of 4 keys x 16 columns, keys 4 h .. and 8 further
+  uint32_t ka[D / 16], va[2][DT];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i)
+    ka[i] = (uint32_t)((wk * KPW * 32 + c) * T::ROW + (((2 * i + h) ^ (c % T::CPR)) << 4));
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+#pragma unroll
+    for (int t = 0; t < DT; ++t) {
+      const int r = wk * KPW * 32 + 8 * e + 4 * h + ((lane & 15) >> 2);
+      const int ch = 4 * t + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      va[e][t] = (uint32_t)(T::KB + r * T::ROW + ((ch ^ (r % T::CPR)) << 4) + (lane & 1) * 8);
+    }
+  // out += V^T P^T over this wave's keys of the stage at `base`
+  auto values = [&](const char* base, const uint4 (&pb)[2 * KPW], f32x16 (&out)[DT]) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < 2 * KPW; ++u)
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
-        const uint16_t* p = vread + 16 * u * LDV + 32 * t;
-        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)p);
-        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + 8 * LDV));
+        const char* p = base + 16 * u * T::ROW;
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + va[0][t]));
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + va[1][t]));
         const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
         out[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(l2.x, l2.y, h2.x, h2.y)), as_bf16x8(pb[u]),
                                                          out[t], 0, 0, 0);
       }
   };
+  // the key of register i of block u
+  auto key_of = [&](int k0, int u, int i) __attribute__((always_inline)) { return k0 + u * 32 + 8 * (i >> 2) + 4 * h + (i & 3); };
+  auto sees = [&](int key) __attribute__((always_inline)) { return (key >= me.lo && key <= me.hi) || key < me.sk; };
 
-  if (tid < 2) odd[tid] = 0;
-  if (t0 < t1) load(w.tile(t0));
-  for (int t = t0; t < t1; ++t) {
-    const int tile = w.tile(t), k0 = tile * KT;
-    // seen whole by every row: inside the window of the first and the last, or among the sinks
-    const bool whole = (s1.lo <= k0 && k0 + KT - 1 <= s0.hi) || k0 + KT <= s0.sk;
-    bool mine = false;
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int at = i * NT + tid, key = at / CH, d = (at % CH) * 8;
-      uint4 v = vr[i];
-      if (!whole) {
-        const bool any = odd_half(v.x) || odd_half(v.y) || odd_half(v.z) || odd_half(v.w);
-        if (any) v = make_uint4(zero_odd(v.x), zero_odd(v.y), zero_odd(v.z), zero_odd(v.w));
-        mine = mine || any;
-      }
-      *reinterpret_cast<uint4*>(Ks + key * LDK + d) = kr[i];
-      *reinterpret_cast<uint4*>(Vs + key * LDV + d) = v;
-    }
-    __syncthreads();
-    // set between a tile's two barriers and read behind the second; the next tile's flag, last read before the
-    // first, is cleared in the same place
-    if (mine) odd[t & 1] = 1;
-    if (tid == 0) odd[(t + 1) & 1] = 0;
-    if (t + 1 < t1) load(w.tile(t + 1));
-
+  // scores, running maximum and sum, values of the wave's keys k0 .. of the stage at `base`
+  auto attend = [&](const char* base, int k0, auto masked) __attribute__((always_inline)) {
     f32x16 sc[KPW];
 #pragma unroll
     for (int u = 0; u < KPW; ++u) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
-      const uint16_t* kread = Ks + ((wk * KPW + u) * 32 + c) * LDK + 8 * h;
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
-        sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(*reinterpret_cast<const uint4*>(kread + 16 * i)),
-                                                        as_bf16x8(qf[i]), sc[u], 0, 0, 0);
+        sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+            as_bf16x8(*reinterpret_cast<const uint4*>(base + u * 32 * T::ROW + ka[i])), as_bf16x8(qf[i]), sc[u], 0, 0, 0);
     }
-    uint32_t sees = 0xffffffffu;                    // bit 16 u + i: register i of block u is a seen key
-    static_assert(KPW <= 2, "one bit per score");
-    if (!whole) {
-      sees = 0;
+    if constexpr (decltype(masked)::value) {
 #pragma unroll
       for (int u = 0; u < KPW; ++u)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = k0 + (wk * KPW + u) * 32 + 8 * (i >> 2) + 4 * h + (i & 3);
-          const bool yes = (key >= me.lo && key <= me.hi) || key < me.sk;
-          sc[u][i] = yes ? sc[u][i] : -INFINITY;
-          sees |= yes ? 1u << (16 * u + i) : 0u;
-        }
+        for (int i = 0; i < 16; ++i) sc[u][i] = sees(key_of(k0, u, i)) ? sc[u][i] : -INFINITY;
     }
     float mx = sc[0][0];
 #pragma unroll
@@ -238,7 +233,7 @@ __global__ __launch_bounds__(64 * WR * WK) void k_attention_masked(AttnArgs g) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c2;
-    if (__any(mx > top)) {
+    if (__any(mx > top + 8.f)) {
       const float next = fmaxf(top, mx);
       const float f = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - next);
       total *= f;
@@ -248,13 +243,13 @@ __global__ __launch_bounds__(64 * WR * WK) void k_attention_masked(AttnArgs g) {
         for (int i = 0; i < 16; ++i) o[d][i] *= f;
       top = next;
     }
-    const float base = top == -INFINITY ? 0.f : top;
+    const float base2 = top == -INFINITY ? 0.f : top;
     uint4 pb[2 * KPW];
 #pragma unroll
     for (int u = 0; u < KPW; ++u) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][i], c2, -base));
+        const float p = __builtin_amdgcn_exp2f(fmaf(sc[u][i], c2, -base2));
         sc[u][i] = p;
         total += p;
       }
@@ -263,105 +258,150 @@ __global__ __launch_bounds__(64 * WR * WK) void k_attention_masked(AttnArgs g) {
         pb[2 * u + e] = make_uint4(f2bf2(sc[u][8 * e], sc[u][8 * e + 1]), f2bf2(sc[u][8 * e + 2], sc[u][8 * e + 3]),
                                    f2bf2(sc[u][8 * e + 4], sc[u][8 * e + 5]), f2bf2(sc[u][8 * e + 6], sc[u][8 * e + 7]));
     }
-    values(pb, o);
-    __syncthreads();
-    if (!whole && odd[t & 1]) {
-      // the tile's value rows held infinities or NaN: their codes take the place of V, the seen keys' ones that of P
-#pragma unroll 1
-      for (int i = 0; i < NL; ++i) {
-        const int at = i * NT + tid, key = tile * KT + at / CH, d = (at % CH) * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (key < kn) v = *reinterpret_cast<const uint4*>(vbase + (int64_t)key * a.vs[1] + d);
-        *reinterpret_cast<uint4*>(Vs + (at / CH) * LDV + d) =
-            make_uint4(odd_codes(v.x), odd_codes(v.y), odd_codes(v.z), odd_codes(v.w));
-      }
-      __syncthreads();
-      f32x16 cnt[DT];
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) cnt[d][i] = 0.f;
-#pragma unroll
-      for (int u = 0; u < 2 * KPW; ++u) {
-        const uint32_t m = sees >> (8 * u);
-        auto pair = [&](int i) { return ((m >> i) & 1 ? 0x3f80u : 0u) | ((m >> (i + 1)) & 1 ? 0x3f800000u : 0u); };
-        pb[u] = make_uint4(pair(0), pair(2), pair(4), pair(6));
-      }
-      values(pb, cnt);
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int v = (int)cnt[d][i];
-          const bool plus = v & 255, minus = (v >> 8) & 255;
-          if (v >= 65536 || (plus && minus)) o[d][i] = NAN;
-          else if (plus) o[d][i] += INFINITY;
-          else if (minus) o[d][i] -= INFINITY;
-        }
-      __syncthreads();
-    }
-  }
+    values(base, pb, o);
+  };
 
-  total += __shfl_xor(total, 32, 64);
-  if constexpr (WK > 1) {
-    // the waves of one set of rows join: maxima and sums first, then the outputs, in wave order
-    float* area = reinterpret_cast<float*>(lds);
-    constexpr int REC = DT * 16 + 2;
-    __syncthreads();
-    if (wk > 0) {
-      float* rec = area + ((wk - 1) * WR + wr) * 64 * REC + lane;
-      rec[0] = top;
-      rec[64] = total;
+  auto walk = [&](auto mode) __attribute__((always_inline)) {
+    constexpr int MODE = decltype(mode)::value;
+    top = -INFINITY;
+    total = 0.f;
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+    for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) rec[(2 + d * 16 + i) * 64] = o[d][i];
+      for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+#pragma unroll
+    for (int i = 0; i < NST - 1; ++i)
+      if (t0 + i < t1) issue(i, w.tile(t0 + i));
+    int slot = 0;
+    for (int t = t0; t < t1; ++t) {
+      // tile t has landed for every wave, and the slot of tile t - 1 is free
+      if (t + NST - 2 < t1) lds_wait_barrier<(NST - 2) * T::LPS>();
+      else lds_wait_barrier<0>();
+      if (t + NST - 1 < t1) issue(slot == 0 ? NST - 1 : slot - 1, w.tile(t + NST - 1));
+      char* base = lds + slot * T::SBYTES;
+      slot = slot + 1 == NST ? 0 : slot + 1;
+      const int k0 = w.tile(t) * KT + wk * KPW * 32, k1 = k0 + KPW * 32;
+      if constexpr (MODE != FAST) {
+        for (int i = tid; i < T::KB / 16; i += 64 * T::NW) {
+          uint4* p = reinterpret_cast<uint4*>(base + T::KB) + i;
+          const uint4 v = *p;
+          *p = MODE == CLEAN ? make_uint4(zero_odd(v.x), zero_odd(v.y), zero_odd(v.z), zero_odd(v.w))
+                             : make_uint4(odd_codes(v.x), odd_codes(v.y), odd_codes(v.z), odd_codes(v.w));
+        }
+        __syncthreads();
+      }
+      if (idle || !((k0 <= v1.hi && k1 > v0.lo) || k0 < v1.sk)) continue;      // none of the wave's rows sees any
+      if constexpr (MODE == COUNT) {
+        f32x16 cnt[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) cnt[d][i] = 0.f;
+        uint4 pb[2 * KPW];
+#pragma unroll
+        for (int u = 0; u < 2 * KPW; ++u) {
+          auto one = [&](int i) __attribute__((always_inline)) { return sees(key_of(k0, u >> 1, 8 * (u & 1) + i)) ? 0x3f80u : 0u; };
+          pb[u] = make_uint4(one(0) | one(1) << 16, one(2) | one(3) << 16, one(4) | one(5) << 16, one(6) | one(7) << 16);
+        }
+        values(base, pb, cnt);
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int v = (int)cnt[d][i];
+            o[d][i] += ((v & 255) ? INFINITY : 0.f) - ((v >> 8 & 255) ? INFINITY : 0.f) + (v >> 16 ? NAN : 0.f);
+          }
+      } else {
+        const bool whole = (v1.lo <= k0 && k1 - 1 <= v0.hi) || k1 <= v0.sk;
+        if (whole) attend(base, k0, std::false_type());
+        else attend(base, k0, std::true_type());
+      }
+    }
+    if constexpr (MODE != COUNT) total += __shfl_xor(total, 32, 64);
+    if constexpr (WK > 1) {
+      // the waves of one set of rows join, in wave order: counts add up, the others at a common reference
+      float* area = reinterpret_cast<float*>(lds);
+      __syncthreads();
+      if (wk > 0) {
+        float* rec = area + ((wk - 1) * WR + wr) * 64 * T::REC + lane;
+        rec[0] = top;
+        rec[64] = total;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) rec[(2 + d * 16 + i) * 64] = o[d][i];
+      }
+      __syncthreads();
+      if (wk == 0) {
+        float next = top;
+#pragma unroll
+        for (int x = 1; x < WK; ++x) next = fmaxf(next, area[((x - 1) * WR + wr) * 64 * T::REC + lane]);
+        const float base2 = next == -INFINITY ? 0.f : next;
+        const float f0 = MODE == COUNT ? 1.f : __builtin_amdgcn_exp2f(top - base2);
+        total *= f0;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] *= f0;
+#pragma unroll
+        for (int x = 1; x < WK; ++x) {
+          const float* rec = area + ((x - 1) * WR + wr) * 64 * T::REC + lane;
+          const float f = MODE == COUNT ? 1.f : __builtin_amdgcn_exp2f(rec[0] - base2);
+          total = fmaf(f, rec[64], total);
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[d][i] = fmaf(f, rec[(2 + d * 16 + i) * 64], o[d][i]);
+        }
+        top = next;
+      }
     }
     __syncthreads();
-    if (wk > 0) return;
-    float next = top;
-#pragma unroll
-    for (int x = 1; x < WK; ++x) next = fmaxf(next, area[((x - 1) * WR + wr) * 64 * REC + lane]);
-    const float base = next == -INFINITY ? 0.f : next;
-    const float f0 = __builtin_amdgcn_exp2f(top - base);
-    total *= f0;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[d][i] *= f0;
-#pragma unroll
-    for (int x = 1; x < WK; ++x) {
-      const float* rec = area + ((x - 1) * WR + wr) * 64 * REC + lane;
-      const float f = __builtin_amdgcn_exp2f(rec[0] - base);
-      total = fmaf(f, rec[64], total);
-#pragma unroll
-      for (int d = 0; d < DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] = fmaf(f, rec[(2 + d * 16 + i) * 64], o[d][i]);
-    }
-    top = next;
-  }
-  if (!live) return;
-  // lane holds columns 32 d + 8 (i / 4) + 4 h + i % 4 of its row
-  if (g.splits > 1) {
-    const int64_t slots = (int64_t)a.batch * a.kv_heads * all, slot = ((int64_t)b * a.kv_heads + hk) * all + row;
-    float* po = g.part + (z * slots + slot) * D + 4 * h;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<float4*>(po + 32 * d + 2 * i) = make_float4(o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]);
-    if (h == 0)
-      *reinterpret_cast<float2*>(g.part + g.splits * slots * D + (z * slots + slot) * 2) = make_float2(top, total);
-    return;
-  }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
+  };
+
+  walk(std::integral_constant<int, FAST>());
+  float chk = 0.f;                                  // NaN if any sum is not finite
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; i += 4)
-      *reinterpret_cast<uint2*>(orow + 32 * d + 2 * i + 4 * h) =
-          make_uint2(f2bf2(o[d][i] * inv, o[d][i + 1] * inv), f2bf2(o[d][i + 2] * inv, o[d][i + 3] * inv));
+    for (int i = 0; i < 16; ++i) chk = fmaf(o[d][i], 0.f, chk);
+  const bool odd = __syncthreads_or(wk == 0 && !(chk == 0.f));
+  if (odd) walk(std::integral_constant<int, CLEAN>());
+
+  // lane holds columns 32 d + 8 (i / 4) + 4 h + i % 4 of its row
+  const int64_t slots = (int64_t)a.batch * a.kv_heads * all, slot = (int64_t)bh * all + row;
+  float* po = g.part + (z * slots + slot) * D + 4 * h;
+  if (wk == 0 && live) {
+    if (g.splits > 1) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<float4*>(po + 32 * d + 2 * i) = make_float4(o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]);
+      if (h == 0)
+        *reinterpret_cast<float2*>(g.part + g.splits * slots * D + (z * slots + slot) * 2) = make_float2(top, total);
+    } else {
+      const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<uint2*>(orow + 32 * d + 2 * i + 4 * h) =
+              make_uint2(f2bf2(o[d][i] * inv, o[d][i + 1] * inv), f2bf2(o[d][i + 2] * inv, o[d][i + 3] * inv));
+    }
+  }
+  if (!odd) return;
+  walk(std::integral_constant<int, COUNT>());
+  if (wk > 0 || !live) return;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (o[d][i] != 0.f) {
+        const int col = 32 * d + 8 * (i >> 2) + (i & 3);
+        if (g.splits > 1) po[col] += o[d][i];
+        else orow[col + 4 * h] = f2bf(bf2f(orow[col + 4 * h]) + o[d][i]);
+      }
 }
 
 // Joins the splits of a row in split order: a wave per row.
@@ -399,13 +439,13 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs g) {
   else *out = f2bf(o[0] * inv);
 }
 
-template <int D, int WR, int WK, int KPW>
+template <int D, int WR, int WK, int KPW, int NST, int MINW>
 hipError_t go(AttnArgs g, hipStream_t s) {
   const int64_t rows = (int64_t)g.a.q_len * g.share;
   g.tiles = (int)((rows + 32 * WR - 1) / (32 * WR));
   const int64_t wgs = (int64_t)g.tiles * g.splits * g.a.kv_heads * g.a.batch;
   if (wgs * 64 * WR * WK >= 1ll << 32) return hipErrorInvalidValue;
-  hipError_t e = launch((k_attention_masked<D, WR, WK, KPW>), dim3((unsigned)wgs), dim3(64 * WR * WK), 0, s, g);
+  hipError_t e = launch((k_attention_masked<D, WR, WK, KPW, NST, MINW>), dim3((unsigned)wgs), dim3(64 * WR * WK), 0, s, g);
   if (e != hipSuccess || g.splits == 1) return e;
   const int64_t slots = rows * g.a.kv_heads * g.a.batch;
   return launch((k_attention_join<D>), dim3((unsigned)((slots + 3) / 4)), dim3(256), 0, s, g);
@@ -445,7 +485,8 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
   g.a = a;
   g.share = a.heads / a.kv_heads;
   const int64_t rows = (int64_t)a.q_len * g.share;
-  if (rows * a.kv_heads * a.batch >= 1ll << 31) return hipErrorInvalidValue;
+  // 32-bit offsets inside a tile of up to 128 keys
+  if (rows * a.kv_heads * a.batch >= 1ll << 31 || a.ks[1] > 1 << 23 || a.vs[1] > 1 << 23) return hipErrorInvalidValue;
   // few rows: the keys are split over workgroups too
   const int wr = rows > 32 ? 4 : 1, kt = wr == 4 ? 64 : 128;
   const int64_t base = (rows + 32 * wr - 1) / (32 * wr) * a.kv_heads * a.batch;
@@ -457,8 +498,8 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
   int64_t z = std::min<int64_t>({512 / base, tiles / 2, fits, 128});
   g.splits = (int)std::max<int64_t>(z, 1);
   g.part = sp.partials;
-  if (a.dim == 64) return wr == 4 ? go<64, 4, 1, 2>(g, s) : go<64, 1, 4, 1>(g, s);
-  return wr == 4 ? go<128, 4, 1, 2>(g, s) : go<128, 1, 4, 1>(g, s);
+  if (a.dim == 64) return wr == 4 ? go<64, 4, 1, 2, 2, 2>(g, s) : go<64, 1, 4, 1, 2, 2>(g, s);
+  return wr == 4 ? go<128, 4, 1, 2, 2, 2>(g, s) : go<128, 1, 4, 1, 2, 1>(g, s);
 }
 
 }  // namespace k

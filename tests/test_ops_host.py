@@ -169,7 +169,7 @@ def attention_args(**kw):
     {"batch": -1}, {"q_len": -1}, {"kv_len": -1}, {"q_len": 1 << 30}, {"kv_len": 1 << 30}, {"heads": 0}, {"kv_heads": 0}, {"kv_heads": 3},
     {"heads": 1 << 17}, {"head_dim": 80}, {"causal": 2}, {"sinks": -1}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")},
     {"work": 0x80}, {"q": None}, {"k": None}, {"v": None}, {"out": None}, {"q": 0x1008}, {"k": 0x2002}, {"v": 0x3008}, {"out": 0x4008},
-    {"q_lens": 0x5002}, {"kv_lens": 0x5001}, {"q_stride": (-8, 256, 64)}, {"k_stride": (2048, 130, 64)}, {"v_stride": (2048, 128, 1 << 41)},
+    {"q_lens": 0x5002}, {"kv_lens": 0x5001}, {"q_stride": (-8, 256, 64)}, {"k_stride": (2048, 130, 64)}, {"v_stride": (2048, 128, 1 << 41)}, {"k_stride": (2048, (1 << 23) + 8, 64)}, {"v_stride": (2048, 1 << 24, 64)},
     {"out_stride": (2048, 256, 56)}, {"out_stride": (0, 256, 64)}, {"batch": 1 << 20, "q_len": 1 << 10}])
 def test_attention_refusals(kw):
     st, msg = _status("tpo_attention", attention_args(**kw))
