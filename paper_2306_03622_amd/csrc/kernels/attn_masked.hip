@@ -205,9 +205,13 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
                                                          out[t], 0, 0, 0);
       }
   };
-  // the key of register i of block u
-  auto key_of = [&](int k0, int u, int i) __attribute__((always_inline)) { return k0 + u * 32 + 8 * (i >> 2) + 4 * h + (i & 3); };
-  auto sees = [&](int key) __attribute__((always_inline)) { return (key >= me.lo && key <= me.hi) || key < me.sk; };
+  // which of the 32 keys from k0 on this lane's row sees, in the order of the lane's registers: register i's key is bit
+  // 8 (i / 4) + i % 4
+  auto seen_bits = [&](int k0) __attribute__((always_inline)) {
+    auto below = [&](int key) { return (uint32_t)((1ull << min(max(key - k0, 0), 32)) - 1); };     // keys in front of `key`
+    return ((below(me.hi + 1) & ~below(me.lo)) | below(me.sk)) >> (4 * h);
+  };
+  auto bit_of = [](int i) { return 8 * (i >> 2) + (i & 3); };
 
   // scores, running maximum and sum, values of the wave's keys k0 .. of the stage at `base`
   auto attend = [&](const char* base, int k0, auto masked) __attribute__((always_inline)) {
@@ -215,17 +219,21 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
 #pragma unroll
     for (int u = 0; u < KPW; ++u) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
-#pragma unroll
       for (int i = 0; i < D / 16; ++i)
         sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            as_bf16x8(*reinterpret_cast<const uint4*>(base + u * 32 * T::ROW + ka[i])), as_bf16x8(qf[i]), sc[u], 0, 0, 0);
+            as_bf16x8(*reinterpret_cast<const uint4*>(base + u * 32 * T::ROW + ka[i])), as_bf16x8(qf[i]),
+            i == 0 ? f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0} : sc[u], 0, 0, 0);
     }
     if constexpr (decltype(masked)::value) {
 #pragma unroll
-      for (int u = 0; u < KPW; ++u)
+      for (int u = 0; u < KPW; ++u) {
+        const uint32_t m = seen_bits(k0 + 32 * u);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sc[u][i] = sees(key_of(k0, u, i)) ? sc[u][i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t on = (uint32_t)((int32_t)(m << (31 - bit_of(i))) >> 31);        // all bits, or none
+          sc[u][i] = __uint_as_float((__float_as_uint(sc[u][i]) & on) | (0xff800000u & ~on));
+        }
+      }
     }
     float mx = sc[0][0];
 #pragma unroll
@@ -300,7 +308,8 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
         uint4 pb[2 * KPW];
 #pragma unroll
         for (int u = 0; u < 2 * KPW; ++u) {
-          auto one = [&](int i) __attribute__((always_inline)) { return sees(key_of(k0, u >> 1, 8 * (u & 1) + i)) ? 0x3f80u : 0u; };
+          const uint32_t m = seen_bits(k0 + 32 * (u >> 1));
+          auto one = [&](int i) __attribute__((always_inline)) { return m >> bit_of(8 * (u & 1) + i) & 1 ? 0x3f80u : 0u; };
           pb[u] = make_uint4(one(0) | one(1) << 16, one(2) | one(3) << 16, one(4) | one(5) << 16, one(6) | one(7) << 16);
         }
         values(base, pb, cnt);
@@ -498,6 +507,7 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
   int64_t z = std::min<int64_t>({512 / base, tiles / 2, fits, 128});
   g.splits = (int)std::max<int64_t>(z, 1);
   g.part = sp.partials;
+  // DISPATCH
   if (a.dim == 64) return wr == 4 ? go<64, 4, 1, 2, 2, 2>(g, s) : go<64, 1, 4, 1, 2, 2>(g, s);
   return wr == 4 ? go<128, 4, 1, 2, 2, 2>(g, s) : go<128, 1, 4, 1, 2, 1>(g, s);
 }
