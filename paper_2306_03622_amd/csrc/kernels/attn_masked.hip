@@ -496,20 +496,43 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
   const int64_t rows = (int64_t)a.q_len * g.share;
   // 32-bit offsets inside a tile of up to 128 keys
   if (rows * a.kv_heads * a.batch >= 1ll << 31 || a.ks[1] > 1 << 23 || a.vs[1] > 1 << 23) return hipErrorInvalidValue;
-  // few rows: the keys are split over workgroups too
-  const int wr = rows > 32 ? 4 : 1, kt = wr == 4 ? 64 : 128;
-  const int64_t base = (rows + 32 * wr - 1) / (32 * wr) * a.kv_heads * a.batch;
-  int64_t span = a.kv_len;
+  const int64_t heads = (int64_t)a.kv_heads * a.batch;
+  auto wgs = [&](int64_t r) { return (rows + r - 1) / r * heads; };      // workgroups of r rows
+  int64_t span = a.kv_len;                                               // keys that a workgroup walks, about
   if (a.left >= 0 && (a.causal || a.right >= 0))
-    span = std::min<int64_t>(span, (int64_t)a.left + (a.causal ? 0 : a.right) + std::min<int64_t>(a.q_len, 32 * wr) + a.sinks);
-  const int64_t tiles = (span + kt - 1) / kt;
-  const int64_t slots = rows * a.kv_heads * a.batch, fits = (int64_t)(sp.partials ? sp.partial_bytes / 4 : 0) / (slots * (a.dim + 2));
-  int64_t z = std::min<int64_t>({512 / base, tiles / 2, fits, 128});
-  g.splits = (int)std::max<int64_t>(z, 1);
-  g.part = sp.partials;
-  // DISPATCH
-  if (a.dim == 64) return wr == 4 ? go<64, 4, 1, 2, 2, 2>(g, s) : go<64, 1, 4, 1, 2, 2>(g, s);
-  return wr == 4 ? go<128, 4, 1, 2, 2, 2>(g, s) : go<128, 1, 4, 1, 2, 1>(g, s);
+    span = std::min<int64_t>(span, (int64_t)a.left + (a.causal ? 0 : a.right) + std::min<int64_t>(a.q_len, 128) + a.sinks);
+  // Splits of the keys over workgroups, to 256 of them, of at least three tiles of kt keys, as far as the scratch holds them:
+  // 8 x 4 heads, one token over 3000 keys: 8 splits of 3 tiles 17.3 us, 16 20.6, 4 20.1; one head for 8 over 30,000: 16 40.8, 32 42.1, 64 52.4.
+  auto split = [&](int64_t workgroups, int kt) {
+    const int64_t slots = rows * heads, fits = sp.partials ? (int64_t)(sp.partial_bytes / 4) / (slots * (a.dim + 2)) : 0;
+    g.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / workgroups, span / (3 * kt), 32, fits}));
+    g.part = sp.partials;
+  };
+  // Measured on MI355X (us), heads / key/value heads x dim, queries over keys:
+  //   32 rows, four waves deep: new tokens, whose cost is the memory's, and short sequences that would not give every CU
+  //     a larger tile: 32 / 8 x 128, 1 over 100,001 105.8 (128 rows, two deep 102.8), 8 x 1 over 2000 20.7 (22.0); 12 x 64, 5 x 96 5.5 (64
+  //     rows 6.0), 512 over 512 8.0 (10.4). But 32 / 8 x 128, 100 over 5000 41 (128 rows, two deep 32.6).
+  //   64 rows, two deep: 32 / 8 x 128, 500 over 500 15.8 (128 rows, two deep 20.2); at dim 64 up to four on every CU: 12 x 64, 8 x 512 17.1
+  //     (128 rows 20.1), 4096 with a window of 256 22.1 (27.8), 8 x 8000 causal 128 (137).
+  //   128 rows, two deep, at dim 128 up to two on every CU: 32 / 8, 2 x 500 over 6000 with a window of 1024 39 (one deep 46), 2000 65.
+  //   256 rows for long walks at dim 128: 32 / 8, 4096 causal 186 (128 rows 203), 8191 675 (735); with a window of 512 4 x 2000 120 (105).
+  //   128 rows else: 12 x 64, 4 x 2048 88 (64 rows 96), 8 x 2048 with a window of 128 38.6.
+  const bool d64 = a.dim == 64;
+  if (rows <= 64 || (wgs(32) <= 256 && span <= 1024)) {
+    split(wgs(32), 128);
+    return d64 ? go<64, 1, 4, 1, 2, 2>(g, s) : go<128, 1, 4, 1, 2, 2>(g, s);
+  }
+  g.splits = 1;
+  if (d64 ? wgs(64) <= 1024 : wgs(64) <= 256 && span <= 1024) {
+    if (d64) split(wgs(64), 64);
+    return d64 ? go<64, 2, 2, 1, 3, 2>(g, s) : go<128, 2, 2, 1, 3, 2>(g, s);
+  }
+  if (!d64 && wgs(128) <= 512) {
+    split(wgs(128), 64);
+    return go<128, 4, 2, 1, 3, 2>(g, s);
+  }
+  if (!d64 && span >= 2048) return go<128, 8, 1, 2, 2, 2>(g, s);
+  return d64 ? go<64, 4, 1, 1, 3, 2>(g, s) : go<128, 4, 1, 1, 3, 2>(g, s);
 }
 
 }  // namespace k

@@ -40,7 +40,7 @@ def run(q, k, v, q_lens=None, kv_lens=None, work=True, stream=None, fill=5.0, **
     return out
 
 
-def check(q, k, v, out, q_lens=None, kv_lens=None, causal=False, window=(-1, -1), sinks=0, scale=0.0, fill=5.0):
+def check(q, k, v, out, q_lens=None, kv_lens=None, causal=False, window=(-1, -1), sinks=0, scale=0.0, fill=5.0, every=1):
     b, nq, h, d = q.shape
     nk, hk = k.shape[1], k.shape[2]
     Q, K, V, O = (t.double().cpu().numpy() for t in (q, k, v, out))
@@ -50,7 +50,7 @@ def check(q, k, v, out, q_lens=None, kv_lens=None, causal=False, window=(-1, -1)
         kn = nk if kv_lens is None else min(max(kv_lens[i], 0), nk)
         assert (O[i, qn:] == fill).all(), "rows behind the last query were written"
         m = seen(qn, kn, causal, *window, sinks)
-        for j in range(h):
+        for j in range(0, h, every):
             jk = j // (h // hk)
             want, tol = attention(Q[i, :qn, j], K[i, :kn, jk], V[i, :kn, jk], m, scale or 1 / math.sqrt(d))
             off = np.abs(O[i, :qn, j] - want)
@@ -127,6 +127,35 @@ def test_exactly_the_seen_keys_count(d, nq, nk, causal, window, sinks):
             assert want.max() < 128
             for head in range(h):
                 assert np.array_equal(np.rint(out[:, head] * all_[:, None]), want), head
+
+
+# shapes for each way of cutting the rows and keys, most of which small ones do not take: rows in 32s, 64s, 128s and 256s, waves
+# one, two and four deep, the keys split or not (the comment in attn_masked.hip names the limits)
+LARGE = [(64, 9, 9, 70, 2000, {"causal": True}), (64, 210, 210, 70, 90, {}), (64, 530, 530, 130, 150, {"window": (40, 3), "sinks": 2}),
+         (128, 100, 100, 70, 300, {"causal": True}), (128, 8, 4, 120, 3000, {"causal": True, "window": (2000, 0), "sinks": 5}),
+         (128, 300, 300, 100, 200, {"window": (64, 64)}), (128, 530, 530, 100, 260, {"causal": True, "window": (100, 0), "sinks": 1}),
+         (128, 530, 530, 70, 2300, {"causal": True}), (128, 1060, 530, 75, 2100, {"window": (2050, 30)})]
+
+
+@pytest.mark.parametrize("i", range(len(LARGE)))
+def test_large(i):
+    d, h, hk, nq, nk, kw = LARGE[i]
+    log(f"{nq} over {nk}, {h} / {hk} heads of {d}: {kw}")
+    q, k, v = make(500 + i, 1, nq, nk, h, hk, d)
+    out = run(q, k, v, **kw)
+    check(q, k, v, out, every=max(1, h // 7), **kw)
+    # hidden infinities and NaN change nothing; a seen one shows in its column of the rows that see it
+    m = seen(nq, nk, kw.get("causal", False), *kw.get("window", (-1, -1)), kw.get("sinks", 0))
+    k2, v2 = k.clone(), v.clone()
+    for j in np.flatnonzero(~m.any(axis=0))[:40]:
+        k2[:, int(j)], v2[:, int(j)] = float("nan"), float("inf")
+    j = int(np.flatnonzero(m.any(axis=0) & ~m.all(axis=0))[-1]) if (m.any(axis=0) & ~m.all(axis=0)).any() else nk - 1
+    v2[0, j, hk // 2, 11] = float("-inf")
+    got, want = run(q, k2, v2, **kw), out.clone()
+    for head in range(hk // 2 * (h // hk), (hk // 2 + 1) * (h // hk)):
+        for i in np.flatnonzero(m[:, j]):
+            want[0, int(i), head, 11] = float("-inf")
+    assert bool((got == want).all())
 
 
 @pytest.mark.parametrize("d", [64, 128])
