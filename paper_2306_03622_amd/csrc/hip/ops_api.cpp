@@ -111,28 +111,26 @@ tp_status tpo_attention(const tpo_attention_args* a, void* stream) {
   for (const void* p : {a->q, a->k, a->v, static_cast<const void*>(a->out)})
     if ((uintptr_t)p % 16) return inval(who, "q, k, v and out must start at 16-byte boundaries");
   if ((uintptr_t)a->q_lens % 4 || (uintptr_t)a->kv_lens % 4) return inval(who, "lengths not aligned to 4 bytes");
-  for (const int64_t* st : {a->q_stride, a->k_stride, a->v_stride, a->out_stride})
-    for (int i = 0; i < 3; ++i)
-      if (st[i] < 0 || st[i] % 8 || st[i] > kMostStride) return inval(who, "strides must be multiples of 8, not negative, below 2^40");
-  if (a->k_stride[1] > 1 << 23 || a->v_stride[1] > 1 << 23) return inval(who, "token strides of k and v must be at most 2^23");
-  {
-    // rows of the output must not share memory
-    const int64_t n[3] = {a->batch, a->q_len, a->heads};
-    for (int i = 0; i < 3; ++i)
-      if (n[i] > 1 && a->out_stride[i] < a->head_dim) return inval(who, "out rows overlap");
-  }
-  if ((int64_t)a->q_len * a->heads * a->batch >= 1ll << 31) return inval(who, "batch * q_len * heads must be below 2^31");
+  // strides of dimensions of one entry are not used
+  const int64_t nq[3] = {a->batch, a->q_len, a->heads}, nk[3] = {a->batch, a->kv_len, a->kv_heads};
   k::Attention g;
+  const struct {
+    const int64_t *from, *n;
+    int64_t* to;
+  } strides[4] = {{a->q_stride, nq, g.qs}, {a->k_stride, nk, g.ks}, {a->v_stride, nk, g.vs}, {a->out_stride, nq, g.os}};
+  for (const auto& st : strides)
+    for (int i = 0; i < 3; ++i) {
+      const int64_t v = st.n[i] > 1 ? st.from[i] : 0;
+      if (v < 0 || v % 8 || v > kMostStride) return inval(who, "strides must be multiples of 8, not negative, below 2^40");
+      if (st.to == g.os && st.n[i] > 1 && v < a->head_dim) return inval(who, "out rows overlap");
+      st.to[i] = v;
+    }
+  if (g.ks[1] > 1 << 23 || g.vs[1] > 1 << 23) return inval(who, "token strides of k and v must be at most 2^23");
+  if ((int64_t)a->q_len * a->heads * a->batch >= 1ll << 31) return inval(who, "batch * q_len * heads must be below 2^31");
   g.q = static_cast<const uint16_t*>(a->q);
   g.k = static_cast<const uint16_t*>(a->k);
   g.v = static_cast<const uint16_t*>(a->v);
   g.out = static_cast<uint16_t*>(a->out);
-  for (int i = 0; i < 3; ++i) {
-    g.qs[i] = a->q_stride[i];
-    g.ks[i] = a->k_stride[i];
-    g.vs[i] = a->v_stride[i];
-    g.os[i] = a->out_stride[i];
-  }
   g.q_lens = a->q_lens;
   g.kv_lens = a->kv_lens;
   g.batch = a->batch; g.heads = a->heads; g.kv_heads = a->kv_heads; g.dim = a->head_dim;

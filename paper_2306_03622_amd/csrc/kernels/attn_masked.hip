@@ -520,12 +520,12 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
   const bool d64 = a.dim == 64;
   if (rows <= 64 || (wgs(32) <= 256 && span <= 1024)) {
     split(wgs(32), 128);
-    return d64 ? go<64, 1, 4, 1, 2, 2>(g, s) : go<128, 1, 4, 1, 2, 2>(g, s);
+    return d64 ? go<64, 1, 4, 1, 2, 2>(g, s) : go<128, 1, 4, 1, 2, 1>(g, s);
   }
   g.splits = 1;
   if (d64 ? wgs(64) <= 1024 : wgs(64) <= 256 && span <= 1024) {
     if (d64) split(wgs(64), 64);
-    return d64 ? go<64, 2, 2, 1, 3, 2>(g, s) : go<128, 2, 2, 1, 3, 2>(g, s);
+    return d64 ? go<64, 2, 2, 1, 3, 2>(g, s) : go<128, 2, 2, 1, 3, 1>(g, s);
   }
   if (!d64 && wgs(128) <= 512) {
     split(wgs(128), 64);

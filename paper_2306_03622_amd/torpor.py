@@ -667,17 +667,14 @@ def tpo_linear_w4(x, weight: W4Weight, out, bias=None, res=None, act: str = "non
         _check(lib(), status)
 
 
-def _strides(name, t, bf, dev):
-    """A [B][tokens][heads][dim] tensor's first three strides, 0 for a dimension of one entry, which is never stepped."""
+def _check_heads(name, t, bf, dev):
+    """Raises for a tensor that attention cannot take."""
     if t.dtype is not bf:
         raise ValueError(f"{name} is {t.dtype}")
     if t.get_device() != dev:
         raise ValueError(f"{name} is on {t.device}, q on device {dev}")
-    s0, s1, s2, s3 = t.stride()
-    if s3 != 1:
+    if t.stride(3) != 1:
         raise ValueError(f"{name}: the values of a head must be contiguous")
-    n0, n1, n2, _ = t.shape
-    return s0 if n0 > 1 else 0, s1 if n1 > 1 else 0, s2 if n2 > 1 else 0
 
 
 def tpo_attention(q, k, v, out, q_lens=None, kv_lens=None, causal: bool = False, window=(-1, -1), sinks: int = 0,
@@ -696,21 +693,30 @@ def tpo_attention(q, k, v, out, q_lens=None, kv_lens=None, causal: bool = False,
         raise ValueError(f"q on {q.device}")
     torch, current, _, call = _ops or _op_calls()
     bf = torch.bfloat16
-    lens = [0, 0]
-    for i, t in enumerate((q_lens, kv_lens)):
-        if t is not None:
-            if t.dtype is not torch.int32 or t.shape != (b,) or not t.is_contiguous() or t.get_device() != dev:
-                raise ValueError(f"{('q_lens', 'kv_lens')[i]} must be a contiguous int32 [{b}] on device {dev}")
-            lens[i] = t.data_ptr()
-    wp = wb = 0
+    q0, q1, q2, q3 = q.stride()
+    k0, k1, k2, k3 = k.stride()
+    v0, v1, v2, v3 = v.stride()
+    o0, o1, o2, o3 = out.stride()
+    if (not (q.dtype is k.dtype is v.dtype is out.dtype is bf) or not (q3 == k3 == v3 == o3 == 1) or
+            not (k.get_device() == v.get_device() == out.get_device() == dev)):
+        for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
+            _check_heads(name, t, bf, dev)
+    ql = kl = wp = wb = 0
+    if q_lens is not None:
+        if q_lens.dtype is not torch.int32 or q_lens.shape != (b,) or not q_lens.is_contiguous() or q_lens.get_device() != dev:
+            raise ValueError(f"q_lens must be a contiguous int32 [{b}] on device {dev}")
+        ql = q_lens.data_ptr()
+    if kv_lens is not None:
+        if kv_lens.dtype is not torch.int32 or kv_lens.shape != (b,) or not kv_lens.is_contiguous() or kv_lens.get_device() != dev:
+            raise ValueError(f"kv_lens must be a contiguous int32 [{b}] on device {dev}")
+        kl = kv_lens.data_ptr()
     if work is not None:
         if work.get_device() != dev:
             raise ValueError(f"work is on {work.device}, q on device {dev}")
         wp, wb = work.data_ptr(), work.numel() * work.element_size()
     left, right = window
-    status = call(_ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), *_strides("q", q, bf, dev),
-                                  *_strides("k", k, bf, dev), *_strides("v", v, bf, dev), *_strides("out", out, bf, dev), *lens,
-                                  b, h, hk, d, nq, nk, causal, left, right, sinks, scale, wp, wb),
+    status = call(_ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), q0, q1, q2, k0, k1, k2, v0, v1, v2,
+                                  o0, o1, o2, ql, kl, b, h, hk, d, nq, nk, causal, left, right, sinks, scale, wp, wb),
                   current(dev) if stream is None else _stream_of(dev, stream))
     if status != TP_OK:
         _check(lib(), status)
