@@ -177,29 +177,27 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
   float top, total;                                 // reference of the exponents (base 2), this lane's half of the sum
   const float c2 = a.scale * 1.44269504088896341f;
 
-  // byte addresses of this lane's fragments inside a stage, for the wave's first 32 keys: K rows, chunk 2 i + h; V^T pieces
-  // of 4 keys x 16 columns, keys 4 h .. and 8 further
-  uint32_t ka[D / 16], va[2][DT];
+  // Byte addresses of this lane's fragments inside a stage, for the wave's first 32 keys: K rows, chunk 2 i + h at ka ^ 32 i; V^T
+  // pieces of 4 keys x 16 columns, columns 32 t at va ^ 64 t, keys 4 h .. and 8 further. (The steps are taken in the loop,
+  // from a register that the compiler cannot see through: kept in registers of their own they drove others out to memory.)
+  const uint32_t ka = (uint32_t)((wk * KPW * 32 + c) * T::ROW + ((h ^ (c % T::CPR)) << 4));
+  uint32_t va[2];
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i)
-    ka[i] = (uint32_t)((wk * KPW * 32 + c) * T::ROW + (((2 * i + h) ^ (c % T::CPR)) << 4));
-#pragma unroll
-  for (int e = 0; e < 2; ++e)
-#pragma unroll
-    for (int t = 0; t < DT; ++t) {
-      const int r = wk * KPW * 32 + 8 * e + 4 * h + ((lane & 15) >> 2);
-      const int ch = 4 * t + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-      va[e][t] = (uint32_t)(T::KB + r * T::ROW + ((ch ^ (r % T::CPR)) << 4) + (lane & 1) * 8);
-    }
+  for (int e = 0; e < 2; ++e) {
+    const int r = wk * KPW * 32 + 8 * e + 4 * h + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    va[e] = (uint32_t)(T::KB + r * T::ROW + ((ch ^ (r % T::CPR)) << 4) + (lane & 1) * 8);
+  }
   // out += V^T P^T over this wave's keys of the stage at `base`
   auto values = [&](const char* base, const uint4 (&pb)[2 * KPW], f32x16 (&out)[DT]) __attribute__((always_inline)) {
+    uint32_t v0a = va[0], v1a = va[1];
+    if constexpr (D > 64) asm volatile("" : "+v"(v0a), "+v"(v1a));
 #pragma unroll
     for (int u = 0; u < 2 * KPW; ++u)
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
         const char* p = base + 16 * u * T::ROW;
-        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + va[0][t]));
-        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + va[1][t]));
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + (v0a ^ (t << 6))));
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + (v1a ^ (t << 6))));
         const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
         out[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(l2.x, l2.y, h2.x, h2.y)), as_bf16x8(pb[u]),
                                                          out[t], 0, 0, 0);
@@ -216,12 +214,14 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
   // scores, running maximum and sum, values of the wave's keys k0 .. of the stage at `base`
   auto attend = [&](const char* base, int k0, auto masked) __attribute__((always_inline)) {
     f32x16 sc[KPW];
+    uint32_t kaddr = ka;
+    if constexpr (D > 64) asm volatile("" : "+v"(kaddr));
 #pragma unroll
     for (int u = 0; u < KPW; ++u) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
         sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            as_bf16x8(*reinterpret_cast<const uint4*>(base + u * 32 * T::ROW + ka[i])), as_bf16x8(qf[i]),
+            as_bf16x8(*reinterpret_cast<const uint4*>(base + u * 32 * T::ROW + (kaddr ^ (i << 5)))), as_bf16x8(qf[i]),
             i == 0 ? f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0} : sc[u], 0, 0, 0);
     }
     if constexpr (decltype(masked)::value) {
