@@ -151,9 +151,9 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
   const Seen v0 = seen_at(a, wrow / g.share + shift, kn);
   const Seen v1 = seen_at(a, (min(wrow + 32, rows) - 1) / g.share + shift, kn);
   const uint16_t* qrow = a.q + (int64_t)b * a.qs[0] + (int64_t)li * a.qs[1] + (int64_t)lh * a.qs[2] + 8 * h;
-  uint4 qf[D / 16];
+  bf16x8 qf[D / 16];
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) qf[i] = *reinterpret_cast<const uint4*>(qrow + 16 * i);
+  for (int i = 0; i < D / 16; ++i) qf[i] = as_bf16x8(*reinterpret_cast<const uint4*>(qrow + 16 * i));
 
   const uint16_t* kbase = a.k + (int64_t)b * a.ks[0] + (int64_t)hk * a.ks[2];
   const uint16_t* vbase = a.v + (int64_t)b * a.vs[0] + (int64_t)hk * a.vs[2];
@@ -178,8 +178,7 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
   const float c2 = a.scale * 1.44269504088896341f;
 
   // Byte addresses of this lane's fragments inside a stage, for the wave's first 32 keys: K rows, chunk 2 i + h at ka ^ 32 i; V^T
-  // pieces of 4 keys x 16 columns, columns 32 t at va ^ 64 t, keys 4 h .. and 8 further. (The steps are taken in the loop,
-  // from a register that the compiler cannot see through: kept in registers of their own they drove others out to memory.)
+  // pieces of 4 keys x 16 columns, columns 32 t at va ^ 64 t, keys 4 h .. and 8 further.
   const uint32_t ka = (uint32_t)((wk * KPW * 32 + c) * T::ROW + ((h ^ (c % T::CPR)) << 4));
   uint32_t va[2];
 #pragma unroll
@@ -189,15 +188,13 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
   }
   // out += V^T P^T over this wave's keys of the stage at `base`
   auto values = [&](const char* base, const uint4 (&pb)[2 * KPW], f32x16 (&out)[DT]) __attribute__((always_inline)) {
-    uint32_t v0a = va[0], v1a = va[1];
-    if constexpr (D > 64) asm volatile("" : "+v"(v0a), "+v"(v1a));
 #pragma unroll
     for (int u = 0; u < 2 * KPW; ++u)
 #pragma unroll
       for (int t = 0; t < DT; ++t) {
         const char* p = base + 16 * u * T::ROW;
-        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + (v0a ^ (t << 6))));
-        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + (v1a ^ (t << 6))));
+        const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + (va[0] ^ (t << 6))));
+        const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p + (va[1] ^ (t << 6))));
         const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
         out[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(make_uint4(l2.x, l2.y, h2.x, h2.y)), as_bf16x8(pb[u]),
                                                          out[t], 0, 0, 0);
@@ -212,19 +209,17 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
   auto bit_of = [](int i) { return 8 * (i >> 2) + (i & 3); };
 
   // scores, running maximum and sum, values of the wave's keys k0 .. of the stage at `base`
-  auto attend = [&](const char* base, int k0, auto masked) __attribute__((always_inline)) {
+  auto attend = [&](const char* base, int k0, bool whole) __attribute__((always_inline)) {
     f32x16 sc[KPW];
-    uint32_t kaddr = ka;
-    if constexpr (D > 64) asm volatile("" : "+v"(kaddr));
 #pragma unroll
     for (int u = 0; u < KPW; ++u) {
 #pragma unroll
       for (int i = 0; i < D / 16; ++i)
         sc[u] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            as_bf16x8(*reinterpret_cast<const uint4*>(base + u * 32 * T::ROW + (kaddr ^ (i << 5)))), as_bf16x8(qf[i]),
+            as_bf16x8(*reinterpret_cast<const uint4*>(base + u * 32 * T::ROW + (ka ^ (i << 5)))), qf[i],
             i == 0 ? f32x16{0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0} : sc[u], 0, 0, 0);
     }
-    if constexpr (decltype(masked)::value) {
+    if (!whole) {
 #pragma unroll
       for (int u = 0; u < KPW; ++u) {
         const uint32_t m = seen_bits(k0 + 32 * u);
@@ -240,7 +235,8 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
     for (int u = 0; u < KPW; ++u)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, sc[u][i]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32, 64)) * c2;
+    const auto half = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+    mx = fmaxf(__uint_as_float(half[0]), __uint_as_float(half[1])) * c2;                 // lanes l and l ^ 32
     if (__any(mx > top + 8.f)) {
       const float next = fmaxf(top, mx);
       const float f = next == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - next);
@@ -280,6 +276,10 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
 #pragma unroll
     for (int i = 0; i < NST - 1; ++i)
       if (t0 + i < t1) issue(i, w.tile(t0 + i));
+    // the queries have arrived: else the compiler, which does not count the loads to LDS, waits for them (and so for the next
+    // tile) in every turn of the loop
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i) asm volatile("" : "+v"(qf[i]));
     int slot = 0;
     for (int t = t0; t < t1; ++t) {
       // tile t has landed for every wave, and the slot of tile t - 1 is free
@@ -322,8 +322,7 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
           }
       } else {
         const bool whole = (v1.lo <= k0 && k1 - 1 <= v0.hi) || k1 <= v0.sk;
-        if (whole) attend(base, k0, std::false_type());
-        else attend(base, k0, std::true_type());
+        attend(base, k0, whole);
       }
     }
     if constexpr (MODE != COUNT) total += __shfl_xor(total, 32, 64);
@@ -509,30 +508,33 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
     g.part = sp.partials;
   };
   // Measured on MI355X (us), heads / key/value heads x dim, queries over keys:
-  //   32 rows, four waves deep: new tokens, whose cost is the memory's, and short sequences that would not give every CU
-  //     a larger tile: 32 / 8 x 128, 1 over 100,001 105.8 (128 rows, two deep 102.8), 8 x 1 over 2000 20.7 (22.0); 12 x 64, 5 x 96 5.5 (64
-  //     rows 6.0), 512 over 512 8.0 (10.4). But 32 / 8 x 128, 100 over 5000 41 (128 rows, two deep 32.6).
-  //   64 rows, two deep: 32 / 8 x 128, 500 over 500 15.8 (128 rows, two deep 20.2); at dim 64 up to four on every CU: 12 x 64, 8 x 512 17.1
-  //     (128 rows 20.1), 4096 with a window of 256 22.1 (27.8), 8 x 8000 causal 128 (137).
-  //   128 rows, two deep, at dim 128 up to two on every CU: 32 / 8, 2 x 500 over 6000 with a window of 1024 39 (one deep 46), 2000 65.
-  //   256 rows for long walks at dim 128: 32 / 8, 4096 causal 186 (128 rows 203), 8191 675 (735); with a window of 512 4 x 2000 120 (105).
-  //   128 rows else: 12 x 64, 4 x 2048 88 (64 rows 96), 8 x 2048 with a window of 128 38.6.
-  const bool d64 = a.dim == 64;
-  if (rows <= 64 || (wgs(32) <= 256 && span <= 1024)) {
+  //   32 rows, four waves deep: few tokens, whose cost is the latency, and short sequences that would not give every CU a larger tile:
+  //     32 / 8 x 128, 8 over 8000 24.5 (64 rows 28.1), 20 over 8000 22.6 (128 rows 31.1), 8 / 1, 1 over 30,000 29.4 (64
+  //     rows 31.7); 12 x 64, 5 x 96 5.3 (5.6), 512 over 512 7.4 (12.6).
+  //   64 rows, two deep, one tile more under way: tokens whose cost is the memory's: 32 / 8 x 128, 1 over 100,001 92.6 (32 rows 97.3), 16 x 1
+  //     with a window of 1024 19.9 (21.1); 12 x 64, 16 x 1 over 3000 36.6 (42.7). Also 32 / 8 x 128, 500 over 500 13.0 (128 rows, two
+  //     deep 22.1); at dim 64 up to four on every CU: 12 x 64, 8 x 512 16.9 (128 rows 18.2), 4096 with a window of 256 19.0 (22.6).
+  //   128 rows, two deep, at dim 128 up to one on every CU: 32 / 8, 2 x 500 over 6000 with a window of 1024 31.0 (one deep 34.4), 100
+  //     over 5000 27.7 (29.0). But 32 / 32, 2 x 1000 53.1 (one deep 44.3).
+  //   256 rows for long walks at dim 128, two on every CU and more: 32 / 8, 4096 causal 150 (128 rows 158), 8191 552 (559).
+  //   128 rows else: 32 / 8 x 128, 4 x 2000 with a window of 512 99 (256 rows 110); 12 x 64, 4 x 2048 70 (64 rows 77), 8 x 2048 with
+  //     a window of 128 37.6 (44.9).
+  const bool d64 = a.dim == 64, heavy = heads * span * a.dim >= 1 << 24;
+  if ((rows <= (d64 ? 64 : 128) && !heavy) || (rows > 64 && wgs(32) <= 256 && span <= 1024)) {
     split(wgs(32), 128);
     return d64 ? go<64, 1, 4, 1, 2, 2>(g, s) : go<128, 1, 4, 1, 2, 1>(g, s);
   }
-  g.splits = 1;
-  if (d64 ? wgs(64) <= 1024 : wgs(64) <= 256 && span <= 1024) {
-    if (d64) split(wgs(64), 64);
+  if (rows <= 64 || (d64 ? wgs(64) <= 1024 : wgs(64) <= 256 && span <= 1024)) {
+    split(wgs(64), 64);
     return d64 ? go<64, 2, 2, 1, 3, 2>(g, s) : go<128, 2, 2, 1, 3, 1>(g, s);
   }
-  if (!d64 && wgs(128) <= 512) {
+  if (!d64 && wgs(128) <= 256) {
     split(wgs(128), 64);
     return go<128, 4, 2, 1, 3, 2>(g, s);
   }
-  if (!d64 && span >= 2048) return go<128, 8, 1, 2, 2, 2>(g, s);
-  return d64 ? go<64, 4, 1, 1, 3, 2>(g, s) : go<128, 4, 1, 1, 3, 2>(g, s);
+  g.splits = 1;
+  if (d64) return go<64, 4, 1, 1, 3, 2>(g, s);
+  return span >= 2048 && wgs(256) >= 512 ? go<128, 8, 1, 2, 2, 2>(g, s) : go<128, 4, 1, 2, 2, 2>(g, s);
 }
 
 }  // namespace k
