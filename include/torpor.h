@@ -44,7 +44,7 @@ enum {
 };
 
 /* TP_W4G*: the weight matrices of the linear layers in 4 bits with a bf16 scale for every 32, 64 or 128 columns of a row
- * (torpor_ops.h), everything else as under TP_BF16 (bf16 inputs, biases, embeddings and LayerNorms). 3.2 to 3.9 times
+ * (torpor_ops.h), everything else as under TP_BF16 (bf16 inputs, biases, embeddings and LayerNorms). 3.6 to 3.9 times
  * fewer bytes of those matrices cross the host link in a cold request. MLP and BERT models whose width, d and ffn are
  * multiples of 128. */
 typedef enum { TP_F32 = 0, TP_BF16 = 1, TP_W4G32 = 2, TP_W4G64 = 3, TP_W4G128 = 4 } tp_dtype;

@@ -13,6 +13,7 @@
  * the parts afterwards. A call uses what fits; with less, or none, it computes the same, slower and in another order
  * of addition. Its contents need no preparation and are undefined afterwards. Calls that may overlap (on
  * different streams, or replays of different graphs) need scratch of their own. TPO_WORK_BYTES is as much as any call uses.
+ * (tpo_attention splits its keys; tpo_linear_w4 splits its columns inside a workgroup and leaves the scratch alone.)
  */
 #ifndef TORPOR_OPS_H
 #define TORPOR_OPS_H
@@ -85,7 +86,8 @@ TP_API tp_status tpo_linear_w4(const tpo_linear_w4_args* a, void* stream);
  * q and out: heads of head_dim (64 or 128) bf16 values; k and v: kv_heads, of which each serves heads / kv_heads
  * consecutive query heads. Strides in elements between sequences, tokens and heads ([0], [1], [2]); the values of a
  * head are contiguous. Every head's values start at a 16-byte boundary (strides are multiples of 8; k's and v's between tokens at most 2^23). A stride of 0
- * (a broadcast input) is allowed except in out; the stride of a dimension of one entry is not used. q_len or batch 0 does nothing. */
+ * (a broadcast input) is allowed except in out; the stride of a dimension of one entry is not used. out's heads overlap
+ * neither each other nor an input. batch * q_len * heads is below 2^30, batch * kv_heads below 2^22. q_len or batch 0 does nothing. */
 typedef struct {
   const void *q, *k, *v;
   void* out;

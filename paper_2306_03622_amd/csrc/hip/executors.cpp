@@ -40,7 +40,7 @@ hipError_t model_linear_w4(ExecCtx& x, uint32_t layer, uint32_t w_role, uint32_t
   a.ldy = a.ldr = a.N;
   a.group = x.m->spec.group;
   a.act = act;
-  return k::linear_w4(a, x.split, x.stream);
+  return k::linear_w4(a, x.stream);
 }
 
 }  // namespace

@@ -91,7 +91,7 @@ tp_status tpo_linear_w4(const tpo_linear_w4_args* a, void* stream) {
   hipStream_t s = static_cast<hipStream_t>(stream);
   OnDeviceOf dev(s);
   if (dev.error != hipSuccess) return done(who, dev.error);
-  return done(who, k::linear_w4(g, scratch(a->work, a->work_bytes), s));
+  return done(who, k::linear_w4(g, s));
 }
 
 tp_status tpo_attention(const tpo_attention_args* a, void* stream) {
@@ -126,7 +126,8 @@ tp_status tpo_attention(const tpo_attention_args* a, void* stream) {
       st.to[i] = v;
     }
   if (g.ks[1] > 1 << 23 || g.vs[1] > 1 << 23) return inval(who, "token strides of k and v must be at most 2^23");
-  if ((int64_t)a->q_len * a->heads * a->batch >= 1ll << 31) return inval(who, "batch * q_len * heads must be below 2^31");
+  if ((int64_t)a->q_len * a->heads * a->batch >= 1ll << 30 || (int64_t)a->batch * a->kv_heads >= 1 << 22)
+    return inval(who, "batch * q_len * heads must be below 2^30, batch * kv_heads below 2^22");
   g.q = static_cast<const uint16_t*>(a->q);
   g.k = static_cast<const uint16_t*>(a->k);
   g.v = static_cast<const uint16_t*>(a->v);

@@ -115,7 +115,7 @@ struct LinearW4 {
   int M = 0, N = 0, K = 0, group = 0;
   int act = 0;                      // ACT_*
 };
-hipError_t linear_w4(const LinearW4& a, const Split& sp, hipStream_t s);
+hipError_t linear_w4(const LinearW4& a, hipStream_t s);
 
 // Attention with lengths, a window and sinks (torpor_ops.h, whose argument block it mirrors). zero_tail: rows behind a
 // sequence's last query are set to zero instead of left.

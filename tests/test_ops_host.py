@@ -170,7 +170,8 @@ def attention_args(**kw):
     {"heads": 1 << 17}, {"head_dim": 80}, {"causal": 2}, {"sinks": -1}, {"scale": -1.0}, {"scale": float("nan")}, {"scale": float("inf")},
     {"work": 0x80}, {"q": None}, {"k": None}, {"v": None}, {"out": None}, {"q": 0x1008}, {"k": 0x2002}, {"v": 0x3008}, {"out": 0x4008},
     {"q_lens": 0x5002}, {"kv_lens": 0x5001}, {"q_stride": (-8, 256, 64)}, {"k_stride": (2048, 130, 64)}, {"v_stride": (2048, 128, 1 << 41)}, {"k_stride": (2048, (1 << 23) + 8, 64)}, {"v_stride": (2048, 1 << 24, 64)},
-    {"out_stride": (2048, 256, 56)}, {"out_stride": (0, 256, 64)}, {"batch": 1 << 20, "q_len": 1 << 10}])
+    {"out_stride": (2048, 256, 56)}, {"out_stride": (0, 256, 64)}, {"batch": 1 << 20, "q_len": 1 << 10},
+    {"batch": 1 << 21, "q_len": 1}])
 def test_attention_refusals(kw):
     st, msg = _status("tpo_attention", attention_args(**kw))
     assert st == tp.TP_E_INVAL and msg.startswith("tpo_attention: "), (st, msg)
