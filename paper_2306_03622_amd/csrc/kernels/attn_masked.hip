@@ -5,7 +5,7 @@
 // query rho / G (G heads per key/value head), so keys and values are read once for all of them. A workgroup
 // takes 32 WR rows (WR waves of 32 side by side, each set WK waves deep over the keys) and walks tiles of 32 KPW WK
 // keys through a ring of NST stages in LDS, filled by loads that go straight there (lds_load16, as in gemm_tile.hpp): rows
-// as they lie in memory, the 16-byte chunk c of a row at position c ^ row, so that the rows read together fall on
+// as they lie in memory, their 16-byte chunks moved (k_at, v_at) so that the rows read together fall on
 // different banks. One barrier per tile; keys beyond the sequence are out of the buffer's bounds and read as zeros.
 //
 // Scores are computed transposed, S^T = K Q^T: lane l holds row l % 32 against keys 8 (i / 4) + 4 (l / 32) + i % 4 in
@@ -94,6 +94,9 @@ struct AttnTile {
   static constexpr int NW = WR * WK, KT = 32 * KPW * WK;
   static constexpr int ROW = 2 * D, CPR = ROW / 16, RPL = 1024 / ROW;          // bytes and chunks of a row, rows a load
   static constexpr int LOADS = KT / RPL / NW, LPS = 2 * LOADS;                 // of K (and of V), in all, per wave
+  // what a row's 16-byte chunks are moved by: K, one chunk of 8 rows read together; V, four chunks of 4 rows
+  __host__ __device__ static constexpr int k_at(int row) { return row % CPR; }
+  __host__ __device__ static constexpr int v_at(int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; }
   static constexpr int KB = KT * ROW, SBYTES = 2 * KB, DT = D / 32;
   static constexpr int REC = DT * 16 + 2;                                      // a lane's results when waves join
   static constexpr int join = (WK - 1) * WR * 64 * REC * 4, lds = NST * SBYTES > join ? NST * SBYTES : join;
@@ -167,9 +170,9 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
 #pragma unroll
     for (int i = 0; i < T::LOADS; ++i) {
       const int r = lrow + i * T::RPL;
-      const uint32_t ch = (uint32_t)((lane % T::CPR) ^ (r % T::CPR)) * 16;
-      lds_load16<false>(rk, dst + i * 1024, r < left ? (uint32_t)r * (uint32_t)(a.ks[1] * 2) + ch : kOffNone, 0);
-      lds_load16<false>(rv, dst + T::KB + i * 1024, r < left ? (uint32_t)r * (uint32_t)(a.vs[1] * 2) + ch : kOffNone, 0);
+      const uint32_t ck = (uint32_t)((lane % T::CPR) ^ T::k_at(r)) * 16, cv = (uint32_t)((lane % T::CPR) ^ T::v_at(r)) * 16;
+      lds_load16<false>(rk, dst + i * 1024, r < left ? (uint32_t)r * (uint32_t)(a.ks[1] * 2) + ck : kOffNone, 0);
+      lds_load16<false>(rv, dst + T::KB + i * 1024, r < left ? (uint32_t)r * (uint32_t)(a.vs[1] * 2) + cv : kOffNone, 0);
     }
   };
 
@@ -179,12 +182,12 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
 
   // Byte addresses of this lane's fragments inside a stage, for the wave's first 32 keys: K rows, chunk 2 i + h at ka ^ 32 i; V^T
   // pieces of 4 keys x 16 columns, columns 32 t at va ^ 64 t, keys 4 h .. and 8 further.
-  const uint32_t ka = (uint32_t)((wk * KPW * 32 + c) * T::ROW + ((h ^ (c % T::CPR)) << 4));
+  const uint32_t ka = (uint32_t)((wk * KPW * 32 + c) * T::ROW + ((h ^ T::k_at(c)) << 4));
   uint32_t va[2];
 #pragma unroll
   for (int e = 0; e < 2; ++e) {
     const int r = wk * KPW * 32 + 8 * e + 4 * h + ((lane & 15) >> 2), ch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    va[e] = (uint32_t)(T::KB + r * T::ROW + ((ch ^ (r % T::CPR)) << 4) + (lane & 1) * 8);
+    va[e] = (uint32_t)(T::KB + r * T::ROW + ((ch ^ T::v_at(r)) << 4) + (lane & 1) * 8);
   }
   // out += V^T P^T over this wave's keys of the stage at `base`
   auto values = [&](const char* base, const uint4 (&pb)[2 * KPW], f32x16 (&out)[DT]) __attribute__((always_inline)) {
@@ -429,17 +432,27 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs g) {
   const int qi = row / g.share, qh = hk * g.share + row - qi * g.share;
   if (qi >= qn) return;
   const float2* ml = reinterpret_cast<const float2*>(g.part + g.splits * slots * D);
-  float top = -INFINITY;
-  for (int z = 0; z < g.splits; ++z) top = fmaxf(top, ml[z * slots + slot].x);
-  const float base = top == -INFINITY ? 0.f : top;
-  float total = 0.f, o[E] = {};
-  for (int z = 0; z < g.splits; ++z) {
-    const float2 v = ml[z * slots + slot];
-    const float f = __builtin_amdgcn_exp2f(v.x - base);
-    total = fmaf(f, v.y, total);
-    const float* p = g.part + (z * slots + slot) * D + lane * E;
+  // lane z holds split z's maximum and sum; the values are read eight splits at a time (one split after the other,
+  // 32 of them for 32 heads took 19 us)
+  const float2 v = lane < g.splits ? ml[lane * slots + slot] : make_float2(-INFINITY, 0.f);
+  float top = v.x;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = fmaf(f, p[e], o[e]);
+  for (int m = 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
+  const float f = __builtin_amdgcn_exp2f(v.x - (top == -INFINITY ? 0.f : top));
+  const float total = wave_sum(f * v.y);
+  float o[E] = {};
+  for (int z0 = 0; z0 < g.splits; z0 += 8) {
+    float p[8][E];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < E; ++e) p[i][e] = g.part[(min(z0 + i, g.splits - 1) * slots + slot) * D + lane * E + e];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float fz = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), min(z0 + i, 63)));
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += z0 + i < g.splits ? fz * p[i][e] : 0.f;
+    }
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;
   uint16_t* out = a.out + (int64_t)b * a.os[0] + (int64_t)qi * a.os[1] + (int64_t)qh * a.os[2] + lane * E;
