@@ -94,8 +94,9 @@ struct AttnTile {
   static constexpr int NW = WR * WK, KT = 32 * KPW * WK;
   static constexpr int ROW = 2 * D, CPR = ROW / 16, RPL = 1024 / ROW;          // bytes and chunks of a row, rows a load
   static constexpr int LOADS = KT / RPL / NW, LPS = 2 * LOADS;                 // of K (and of V), in all, per wave
-  // what a row's 16-byte chunks are moved by: K, one chunk of 8 rows read together; V, four chunks of 4 rows
-  __host__ __device__ static constexpr int k_at(int row) { return row % CPR; }
+  // what a row's 16-byte chunks are moved by: of K one chunk of 16 rows is read together, of V four chunks of 4 rows, 256 bytes
+  // each time, one from each bank
+  __host__ __device__ static constexpr int k_at(int row) { return D == 128 ? row % 16 : row / 2 % 8; }
   __host__ __device__ static constexpr int v_at(int row) { return D == 128 ? (row & 3) << 2 : (row & 2) << 1; }
   static constexpr int KB = KT * ROW, SBYTES = 2 * KB, DT = D / 32;
   static constexpr int REC = DT * 16 + 2;                                      // a lane's results when waves join
