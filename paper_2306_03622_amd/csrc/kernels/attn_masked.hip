@@ -528,11 +528,12 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
   //   64 rows, two deep, one tile more under way: tokens whose cost is the memory's: 32 / 8 x 128, 1 over 100,001 92.6 (32 rows 97.3), 16 x 1
   //     with a window of 1024 19.9 (21.1); 12 x 64, 16 x 1 over 3000 36.6 (42.7). Also 32 / 8 x 128, 500 over 500 13.0 (128 rows, two
   //     deep 22.1); at dim 64 up to four on every CU: 12 x 64, 8 x 512 16.9 (128 rows 18.2), 4096 with a window of 256 19.0 (22.6).
-  //   128 rows, two deep, at dim 128 up to one on every CU: 32 / 8, 2 x 500 over 6000 with a window of 1024 31.0 (one deep 34.4), 100
-  //     over 5000 27.7 (29.0). But 32 / 32, 2 x 1000 53.1 (one deep 44.3).
+  //   128 rows, two deep, 64 keys a wave, at dim 128 up to one on every CU: 32 / 8, 2 x 500 over 6000 with a window of 1024 30.8 (one deep
+  //     34.4), 100 over 5000 24.8 (29.0). But 32 / 32, 2 x 1000 53.1 (one deep 44.3).
   //   256 rows for long walks at dim 128, two on every CU and more: 32 / 8, 4096 causal 150 (128 rows 158), 8191 552 (559).
-  //   128 rows else: 32 / 8 x 128, 4 x 2000 with a window of 512 99 (256 rows 110); 12 x 64, 4 x 2048 70 (64 rows 77), 8 x 2048 with
-  //     a window of 128 37.6 (44.9).
+  //   128 rows else: 32 / 8 x 128, 4 x 2000 with a window of 512 99 (256 rows 110); 12 x 64, 8 x 2048 with
+  //     a window of 128 34.5 (64 rows 45). There 32 keys a wave, but 64 on long walks: 8000 causal 153 (32 keys 168), 4 x 2048 78 (85);
+  //     with the window 36.
   const bool d64 = a.dim == 64, heavy = heads * span * a.dim >= 1 << 24;
   if ((rows <= (d64 ? 64 : 128) && !heavy) || (rows > 64 && wgs(32) <= 256 && span <= 1024)) {
     split(wgs(32), 128);
@@ -543,11 +544,11 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
     return d64 ? go<64, 2, 2, 1, 3, 2>(g, s) : go<128, 2, 2, 1, 3, 1>(g, s);
   }
   if (!d64 && wgs(128) <= 256) {
-    split(wgs(128), 64);
-    return go<128, 4, 2, 1, 3, 2>(g, s);
+    split(wgs(128), 128);
+    return go<128, 4, 2, 2, 2, 2>(g, s);
   }
   g.splits = 1;
-  if (d64) return go<64, 4, 1, 1, 3, 2>(g, s);
+  if (d64) return span >= 1024 ? go<64, 4, 1, 2, 2, 2>(g, s) : go<64, 4, 1, 1, 3, 2>(g, s);
   return span >= 2048 && wgs(256) >= 512 ? go<128, 8, 1, 2, 2, 2>(g, s) : go<128, 4, 1, 2, 2, 2>(g, s);
 }
 
