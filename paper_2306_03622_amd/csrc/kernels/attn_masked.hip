@@ -514,11 +514,12 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
   int64_t span = a.kv_len;                                               // keys that a workgroup walks, about
   if (a.left >= 0 && (a.causal || a.right >= 0))
     span = std::min<int64_t>(span, (int64_t)a.left + (a.causal ? 0 : a.right) + std::min<int64_t>(a.q_len, 128) + a.sinks);
-  // Splits of the keys over workgroups, to 256 of them, of at least three tiles of kt keys, as far as the scratch holds them:
-  // 8 x 4 heads, one token over 3000 keys: 8 splits of 3 tiles 17.3 us, 16 20.6, 4 20.1; one head for 8 over 30,000: 16 40.8, 32 42.1, 64 52.4.
+  // Splits of the keys over workgroups, to 256 of them, of at least three tiles of kt keys, as far as the scratch holds them (a
+  // lane of the joining wave for each). One token, 8 / 1 heads of 128 over 30,000 keys: 64 splits 17.9 us, 32 19.4, 16 25.2, none 240;
+  // 32 / 8 over 8000: 20 splits 16.2, 8 18.4; 8 x 32 / 8 over 3000: 8 splits 24.0, 16 27.7; ten over 600, 12 of 64: none 7.5, four 9.2.
   auto split = [&](int64_t workgroups, int kt) {
     const int64_t slots = rows * heads, fits = sp.partials ? (int64_t)(sp.partial_bytes / 4) / (slots * (a.dim + 2)) : 0;
-    g.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / workgroups, span / (3 * kt), 32, fits}));
+    g.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / workgroups, span / (3 * kt), 64, fits}));
     g.part = sp.partials;
   };
   // Measured on MI355X (us), heads / key/value heads x dim, queries over keys:
