@@ -272,6 +272,14 @@ __global__ __launch_bounds__(64 * WGN * WGM * KS, MINW) void k_w4_tile(W4Args g,
     const int kb = st * KS + ks;
     const uint32_t dst = lds0 + slot * T::SBYTES + ks * T::BLOCK;
     const int left = a.K - kb * 128;              // columns from here to the end
+    if (left >= 128) {
+#pragma unroll
+      for (int t = 0; t < T::TX; ++t) lds_load16<false>(rx, dst + (wave * T::TX + t) * 1024, offx[t], kb * 256);
+#pragma unroll
+      for (int t = 0; t < T::TW; ++t) lds_load16<false>(rw, dst + T::XB + (wave * T::TW + t) * 1024, offw[t], kb * 1024);
+      lds_load16<false>(rs, dst + T::XB + T::WB + (wave % T::SPARTS) * 1024, offs, kb * GP * 32);
+      return;
+    }
     const bool in = left > 0;
 #pragma unroll
     for (int t = 0; t < T::TX; ++t)
