@@ -573,7 +573,8 @@ _ops = None
 
 
 def _op_calls():
-    """(torch, its raw current stream by device, tpo_linear_w4, tpo_attention), the last two on packed arguments."""
+    """(torch, its raw current stream by device, its current device, tpo_linear_w4, tpo_attention), the last two on packed
+    arguments."""
     global _ops
     if _ops is None:
         import torch
@@ -583,7 +584,7 @@ def _op_calls():
             f = L[name]                   # a function object of its own
             f.argtypes, f.restype = [C.c_char_p, _P], C.c_int32
             calls.append(f)
-        _ops = (torch, torch._C._cuda_getCurrentRawStream, *calls)
+        _ops = (torch, torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, *calls)
     return _ops
 
 
@@ -593,6 +594,12 @@ def _stream_of(device, stream):
     if owner is not None and owner.index != device:
         raise ValueError(f"stream of {owner}, tensors on device {device}")
     return _ptr(stream)
+
+
+def _call_on(call, packed, device, stream):
+    """The call's status, made with the tensors' device the current one."""
+    with _ops[0].cuda.device(device):
+        return call(packed, stream)
 
 
 class W4Weight:
@@ -637,7 +644,7 @@ def _check_rows(name, t, rows, cols, dtypes, device):
 def tpo_linear_w4(x, weight: W4Weight, out, bias=None, res=None, act: str = "none", work=None, stream=None):
     """out = act(x W^T + bias + res): x, res bf16 [M][K] and [M][N], out bf16 or fp32 [M][N], bias bf16 [N], all on the
     weight's device. stream: a torch stream of that device (default: its current one); work: a uint8 tensor of scratch."""
-    torch, current, call, _ = _ops or _op_calls()
+    torch, current, here, call, _ = _ops or _op_calls()
     bf = torch.bfloat16
     dev, codes, scales = weight._packed
     n, k = weight.out_features, weight.in_features
@@ -660,9 +667,11 @@ def tpo_linear_w4(x, weight: W4Weight, out, bias=None, res=None, act: str = "non
         if work.get_device() != dev:
             raise ValueError(f"work is on {work.device}, the weight on device {dev}")
         wp, wb = work.data_ptr(), work.numel() * work.element_size()
-    status = call(_LINEAR.pack(x.data_ptr(), ldx, codes, scales, bp, rp, ldr, out.data_ptr(), ldy, TP_F32 if f32 else TP_BF16,
-                               m, n, k, weight.group, TP_ACT[act], wp, wb),
-                  current(dev) if stream is None else _stream_of(dev, stream))
+    packed = _LINEAR.pack(x.data_ptr(), ldx, codes, scales, bp, rp, ldr, out.data_ptr(), ldy, TP_F32 if f32 else TP_BF16, m, n, k,
+                          weight.group, TP_ACT[act], wp, wb)
+    s = current(dev) if stream is None else _stream_of(dev, stream)
+    # the null stream is that of whichever device is current; any other carries its own
+    status = call(packed, s) if s or here() == dev else _call_on(call, packed, dev, s)
     if status != TP_OK:
         _check(lib(), status)
 
@@ -691,7 +700,7 @@ def tpo_attention(q, k, v, out, q_lens=None, kv_lens=None, causal: bool = False,
     dev = q.get_device()
     if dev < 0:
         raise ValueError(f"q on {q.device}")
-    torch, current, _, call = _ops or _op_calls()
+    torch, current, here, _, call = _ops or _op_calls()
     bf = torch.bfloat16
     q0, q1, q2, q3 = q.stride()
     k0, k1, k2, k3 = k.stride()
@@ -715,9 +724,10 @@ def tpo_attention(q, k, v, out, q_lens=None, kv_lens=None, causal: bool = False,
             raise ValueError(f"work is on {work.device}, q on device {dev}")
         wp, wb = work.data_ptr(), work.numel() * work.element_size()
     left, right = window
-    status = call(_ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), q0, q1, q2, k0, k1, k2, v0, v1, v2,
-                                  o0, o1, o2, ql, kl, b, h, hk, d, nq, nk, causal, left, right, sinks, scale, wp, wb),
-                  current(dev) if stream is None else _stream_of(dev, stream))
+    packed = _ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), q0, q1, q2, k0, k1, k2, v0, v1, v2, o0, o1, o2,
+                             ql, kl, b, h, hk, d, nq, nk, causal, left, right, sinks, scale, wp, wb)
+    s = current(dev) if stream is None else _stream_of(dev, stream)
+    status = call(packed, s) if s or here() == dev else _call_on(call, packed, dev, s)
     if status != TP_OK:
         _check(lib(), status)
 

@@ -132,7 +132,7 @@ def test_exactly_the_seen_keys_count(d, nq, nk, causal, window, sinks):
 # shapes for each way of cutting the rows and keys, most of which small ones do not take: rows in 32s, 64s, 128s and 256s, waves
 # one, two and four deep, the keys split or not (the comment in attn_masked.hip names the limits)
 LARGE = [(64, 9, 9, 70, 2000, {"causal": True}), (64, 530, 530, 130, 1100, {"causal": True, "window": (1040, 0), "sinks": 3}), (64, 210, 210, 70, 90, {}), (64, 530, 530, 130, 150, {"window": (40, 3), "sinks": 2}),
-         (128, 100, 100, 70, 300, {"causal": True}), (128, 8, 4, 120, 3000, {"causal": True, "window": (2000, 0), "sinks": 5}),
+         (128, 100, 100, 70, 300, {"causal": True}), (128, 60, 60, 150, 300, {"causal": True}), (128, 8, 4, 120, 3000, {"causal": True, "window": (2000, 0), "sinks": 5}),
          (128, 300, 300, 100, 200, {"window": (64, 64)}), (128, 530, 530, 100, 260, {"causal": True, "window": (100, 0), "sinks": 1}),
          (128, 530, 530, 70, 2300, {"causal": True}), (128, 1060, 530, 75, 2100, {"window": (2050, 30)}),
          (64, 16, 8, 3, 33000, {"causal": True}), (128, 32, 8, 2, 17000, {"causal": True, "window": (16500, 0), "sinks": 9})]
