@@ -54,6 +54,12 @@ __device__ __forceinline__ bf16x8 w4_surplus() {
   return as_bf16x8(make_uint4(0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u, 0xC1C0C1C0u));
 }
 
+// ReLU of what is not a number is not one either (act_apply gives 0): a row that an infinite or NaN input has spoilt shows it.
+__device__ __forceinline__ float w4_act(float v, int act) {
+  if (act == ACT_RELU) return v <= 0.f ? 0.f : v;
+  return act_apply(v, act);
+}
+
 // outputs n0 .. n0 + 3 of row m
 __device__ __forceinline__ void w4_store(const W4Args& g, int m, int n0, f32x4 acc) {
   const LinearW4& a = g.a;
@@ -70,7 +76,7 @@ __device__ __forceinline__ void w4_store(const W4Args& g, int m, int n0, f32x4 a
       v[0] += bf2f(w.x & 0xffff); v[1] += bf2f(w.x >> 16); v[2] += bf2f(w.y & 0xffff); v[3] += bf2f(w.y >> 16);
     }
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = act_apply(v[e], a.act);
+    for (int e = 0; e < 4; ++e) v[e] = w4_act(v[e], a.act);
     if (a.y_f32) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + at) = make_float4(v[0], v[1], v[2], v[3]);
     else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + at) = make_uint2(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]));
     return;
@@ -81,7 +87,7 @@ __device__ __forceinline__ void w4_store(const W4Args& g, int m, int n0, f32x4 a
     float t = v[e];
     if (a.bias) t += bf2f(a.bias[n0 + e]);
     if (a.res) t += bf2f(a.res[(int64_t)m * a.ldr + n0 + e]);
-    t = act_apply(t, a.act);
+    t = w4_act(t, a.act);
     if (a.y_f32) static_cast<float*>(a.y)[at + e] = t;
     else static_cast<uint16_t*>(a.y)[at + e] = f2bf(t);
   }
