@@ -54,8 +54,8 @@ TP_API tp_status tpo_w4_quantize(const float* w, int32_t N, int32_t K, int32_t g
  * x, res bf16, y bf16 or fp32 (y_dtype), rows ldx, ldr and ldy elements apart; bias bf16 or NULL, res or NULL. Products
  * and sums are exact bf16 products in fp32 sums, scales applied to each group's sum, one rounding at the end.
  * x starts at a 16-byte boundary and ldx is a multiple of 8 below 2^23; wq and scales start at 16-byte boundaries. y may
- * be res (same ldr and ldy, both bf16); apart from that outputs do not overlap inputs. M = 0 does nothing. An infinite
- * x[m][k] makes row m NaN. */
+ * be res (same ldr and ldy, both bf16); apart from that outputs do not overlap inputs. M = 0 does nothing. M in whole 128s
+ * times N in whole 256s is below 2^38. An infinite x[m][k] makes row m NaN. */
 typedef struct {
   const void* x;
   int64_t ldx;

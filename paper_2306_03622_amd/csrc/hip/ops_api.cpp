@@ -74,6 +74,8 @@ tp_status tpo_linear_w4(const tpo_linear_w4_args* a, void* stream) {
     return inval(who, "y, bias or res not aligned to its element");
   if (a->ldx < a->K || a->ldy < a->N || (a->res && a->ldr < a->N)) return inval(who, "a row stride below the row's length");
   if (a->ldx >= 1 << 23 || a->ldy > kMostStride || (a->res && a->ldr > kMostStride)) return inval(who, "row stride too large");
+  if (((int64_t)a->M + 127) / 128 * ((a->N + 255) / 256) >= 1 << 23)
+    return inval(who, "M in whole 128s times N in whole 256s must be below 2^38");
   if (a->res == a->y && (a->y_dtype != TP_BF16 || a->ldr != a->ldy))
     return inval(who, "y may be res only in bf16 and with the same row stride");
   k::LinearW4 g;

@@ -360,9 +360,7 @@ template <int BN, int BM, int WGN, int WGM, int KS, int NST, int MINW>
 hipError_t go_tile(const W4Args& g, hipStream_t s) {
   constexpr int threads = 64 * WGN * WGM * KS;
   const int tn = (g.a.N + BN - 1) / BN, tm = (g.a.M + BM - 1) / BM;
-  const int64_t tiles = (int64_t)tn * tm;
-  if (tiles * threads >= 1ll << 32) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)tiles), block(threads);
+  const dim3 grid((unsigned)tn * tm), block(threads);
   switch (g.a.group) {
     case 128: return launch((k_w4_tile<BN, BM, WGN, WGM, KS, NST, 1, MINW>), grid, block, 0, s, g, tn, tm);
     case 64: return launch((k_w4_tile<BN, BM, WGN, WGM, KS, NST, 2, MINW>), grid, block, 0, s, g, tn, tm);
@@ -374,7 +372,6 @@ template <int MT, int NB, int NW, int U>
 hipError_t go_rows(const W4Args& g, hipStream_t s) {
   const int nbs = (g.a.N + 15) / 16;
   const dim3 grid((nbs + NB - 1) / NB, (g.a.M + 16 * MT - 1) / (16 * MT)), block(64 * NW);
-  if (grid.y > 65535) return hipErrorInvalidValue;
   switch (g.a.group) {
     case 128: return launch((k_w4_rows<MT, NB, NW, 1, U>), grid, block, 0, s, g);
     case 64: return launch((k_w4_rows<MT, NB, NW, 2, U>), grid, block, 0, s, g);
@@ -407,7 +404,8 @@ hipError_t linear_w4(const LinearW4& a, hipStream_t s) {
     case W4_TILE64X64: return go_tile<64, 64, 2, 2, 1, 2, 2>(g, s);
     case W4_TILE128X64: return go_tile<128, 64, 4, 2, 1, 2, 2>(g, s);
     case W4_TILE128X64_WIDE: return go_tile<128, 64, 4, 1, 1, 2, 2>(g, s);
-    default: return go_tile<256, 128, 4, 2, 1, 3, 2>(g, s);
+    case W4_TILE256X128: return go_tile<256, 128, 4, 2, 1, 3, 2>(g, s);
+    default: return hipErrorInvalidValue;        // no variant's grid holds so many outputs
   }
 }
 
