@@ -664,8 +664,8 @@ def tpo_linear_w4(x, weight: W4Weight, out, bias=None, res=None, act: str = "non
         _check_rows("res", res, m, n, (bf,), dev)
         rp, ldr = res.data_ptr(), res.stride(0) if m > 1 else n
     if work is not None:
-        if work.get_device() != dev:
-            raise ValueError(f"work is on {work.device}, the weight on device {dev}")
+        if work.get_device() != dev or not work.is_contiguous():
+            raise ValueError(f"work must be contiguous and on device {dev}, not {tuple(work.shape)} by {work.stride()} on {work.device}")
         wp, wb = work.data_ptr(), work.numel() * work.element_size()
     packed = _LINEAR.pack(x.data_ptr(), ldx, codes, scales, bp, rp, ldr, out.data_ptr(), ldy, TP_F32 if f32 else TP_BF16, m, n, k,
                           weight.group, TP_ACT[act], wp, wb)
@@ -720,8 +720,8 @@ def tpo_attention(q, k, v, out, q_lens=None, kv_lens=None, causal: bool = False,
             raise ValueError(f"kv_lens must be a contiguous int32 [{b}] on device {dev}")
         kl = kv_lens.data_ptr()
     if work is not None:
-        if work.get_device() != dev:
-            raise ValueError(f"work is on {work.device}, q on device {dev}")
+        if work.get_device() != dev or not work.is_contiguous():
+            raise ValueError(f"work must be contiguous and on device {dev}, not {tuple(work.shape)} by {work.stride()} on {work.device}")
         wp, wb = work.data_ptr(), work.numel() * work.element_size()
     left, right = window
     packed = _ATTENTION.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), q0, q1, q2, k0, k1, k2, v0, v1, v2, o0, o1, o2,
