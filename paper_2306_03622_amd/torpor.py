@@ -603,7 +603,11 @@ def _call_on(call, packed, device, stream):
 
 
 class W4Weight:
-    """A matrix W[N][K] in 4 bits on the device: codes (uint8) and scales (bf16) in blocked order."""
+    """A matrix W[N][K] in 4 bits on the device: codes (uint8) and scales (bf16) in blocked order. It shares the memory of the
+    tensors it is made from and keeps that memory, so values written there later are the matrix's. Nothing else of it
+    changes: a call goes by the addresses taken here."""
+
+    __slots__ = ("_codes", "_scales", "_packed", "device", "out_features", "in_features", "group")
 
     def __init__(self, codes, scales, out_features: int, in_features: int, group: int):
         import torch
@@ -616,9 +620,20 @@ class W4Weight:
             raise ValueError("codes and scales must be contiguous")
         if codes.device.type != "cuda" or scales.device != codes.device:
             raise ValueError(f"codes on {codes.device}, scales on {scales.device}")
-        self.codes, self.scales, self.device = codes, scales, codes.device
-        self._packed = (codes.device.index, codes.data_ptr(), scales.data_ptr())
-        self.out_features, self.in_features, self.group = out_features, in_features, group
+        # tensor objects of its own hold the memory: the caller's may be given other memory (t.data = ..)
+        for name, value in (("_codes", codes.detach()), ("_scales", scales.detach()), ("device", codes.device),
+                            ("_packed", (codes.device.index, codes.data_ptr(), scales.data_ptr())),
+                            ("out_features", out_features), ("in_features", in_features), ("group", group)):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"{name} of a W4Weight is fixed: make another one")
+
+    def __reduce__(self):                 # copies and pickles: made anew from its tensors
+        return W4Weight, (self._codes, self._scales, self.out_features, self.in_features, self.group)
+
+    codes = property(lambda self: self._codes.detach())
+    scales = property(lambda self: self._scales.detach())
 
     @classmethod
     def from_plain(cls, codes: np.ndarray, scales: np.ndarray, group: int, device="cuda"):

@@ -1,5 +1,6 @@
 """What the operators' binding hands to the library (no GPU: the library's calls are recorded, not made)."""
 import contextlib
+import copy
 import types
 
 import pytest
@@ -61,3 +62,36 @@ def test_scratch_is_the_memory_of_its_tensor(op, calls):
     assert len(calls) == 1 and len(calls[0]) == packer.size
     a = layout.from_buffer_copy(calls[0])
     assert a.work == one.data_ptr() + 256 and a.work_bytes == 4096 - 256
+
+
+class Device(torch.Tensor):
+    """A host tensor whose device is said to be a GPU's."""
+
+    device = property(lambda self: types.SimpleNamespace(type="cuda", index=1))
+
+    def __deepcopy__(self, memo):
+        return self.as_subclass(torch.Tensor).clone().as_subclass(Device)
+
+
+def test_a_weight_keeps_the_memory_that_its_calls_read(calls):
+    codes, scales = torch.zeros(2048, dtype=torch.uint8), torch.zeros(32, dtype=torch.bfloat16)
+    was = codes.data_ptr(), scales.data_ptr()
+    mine = codes.as_subclass(Device), scales.as_subclass(Device)
+    w = T.W4Weight(*mine, 32, 128, 128)
+    other = torch.ones(2048, dtype=torch.uint8), torch.ones(32, dtype=torch.bfloat16)
+    for name, value in (("codes", other[0]), ("scales", other[1]), ("out_features", 4096), ("in_features", 256), ("group", 32),
+                        ("device", None), ("_packed", (0, 0, 0))):
+        with pytest.raises(AttributeError):
+            setattr(w, name, value)
+    for t, o in zip((*mine, w.codes, w.scales, codes, scales), (*other, *other, *other)):
+        t.data = o                       # gives the tensor object other memory; the weight's stays, and so does its own object
+    T.tpo_linear_w4(rows(3, 128), w, rows(3, 32))
+    a = T.tpo_linear_w4_args.from_buffer_copy(calls[0])
+    assert (a.wq, a.scales) == was and (a.N, a.K, a.group) == (32, 128, 128)
+    assert (w.codes.data_ptr(), w.scales.data_ptr()) == was
+    assert w.codes.numel() == 2048 and not bool(w.codes.any())      # the memory is still there, as it was
+    for make, shares in ((copy.copy, True), (copy.deepcopy, False)):
+        c = make(w)
+        assert (c._packed == w._packed) == shares and c._packed[1] == c.codes.data_ptr() and c.out_features == 32
+    w._codes.fill_(3)
+    assert bool((w.codes == 3).all())
