@@ -143,10 +143,23 @@ hipError_t linear_bf16(const uint16_t* x, int M, int K, const uint16_t* w, int N
     hipError_t e = launch_skinny(a, s);
     return e == hipSuccess ? finish(a, s) : e;
   }
-  // the tiled kernel addresses x and w through 32-bit buffer offsets, and loads them straight into LDS
+  // the tiled kernel addresses x, w and the residual through 32-bit buffer offsets, and loads x and w straight into LDS
   // in 16-byte pieces, from 16-byte boundaries only
-  if ((size_t)M * K * 2 >= (1u << 31) || (size_t)N * K * 2 >= (1u << 31) || ((uintptr_t)x & 15) || ((uintptr_t)w & 15))
-    return hipErrorInvalidValue;
+  if ((size_t)N * K * 2 >= (1u << 31) || ((uintptr_t)x & 15) || ((uintptr_t)w & 15)) return hipErrorInvalidValue;
+  const int64_t rows = rows_a_launch(M, K, ep.res ? N : 0);
+  if (rows < 1) return hipErrorInvalidValue;
+  if (rows < M) {                          // x or the residual of 2 GiB and more: one range of rows after the other
+    for (int64_t m = 0; m < M; m += rows) {
+      Epilogue e = ep;
+      auto at = [&](const void* p, int f32) { return p ? (char*)p + m * N * (f32 ? 4 : 2) : nullptr; };
+      e.res = at(ep.res, 0);
+      e.out = at(ep.out, ep.out_f32);
+      e.ln_out = at(ep.ln_out, ep.ln_out_f32);
+      const hipError_t err = linear_bf16(x + m * K, (int)std::min<int64_t>(rows, M - m), K, w, N, e, sp, s);
+      if (err != hipSuccess) return err;
+    }
+    return hipSuccess;
+  }
   return pick_tiled<X_ROWS>(a, sp, s);
 }
 

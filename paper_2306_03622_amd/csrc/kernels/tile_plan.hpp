@@ -45,6 +45,17 @@ TP_HOST_DEVICE TileAt tile_at(int id, int total, int tn, int tm, int splits) {
   return t;
 }
 
+// Rows that a launch of a linear layer takes, of M: all while they are below 2 GiB of x (K bf16 values) and of the residual (N, 0:
+// there is none), whose bytes the kernel counts in 32 bits; else M in equal parts, of whole 256s, that are. 0: not even 256 fit.
+inline long rows_a_launch(long M, long K, long N) {
+  const long wide = 2 * std::max(K, N), most = ((1l << 31) - 1) / wide;
+  if (M <= most) return M;
+  const long whole = most / 256 * 256;
+  if (whole == 0) return 0;
+  const long parts = (M + whole - 1) / whole;
+  return ((M + parts - 1) / parts + 255) / 256 * 256;
+}
+
 // y[M][N] = x[M][K] w[N][K]^T; conv: an implicit-GEMM convolution; gelu, ln: the epilogue has a GELU, a row
 // LayerNorm follows; far: the weights are read over the host link
 struct TileShape {
