@@ -452,7 +452,8 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs g) {
     for (int i = 0; i < 8; ++i) {
       const float fz = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), min(z0 + i, 63)));
 #pragma unroll
-      for (int e = 0; e < E; ++e) o[e] += z0 + i < g.splits ? fz * p[i][e] : 0.f;
+      for (int e = 0; e < E; ++e)      // an infinity (of a seen value) stays one where its split weighs next to nothing
+        o[e] += z0 + i < g.splits ? (fabsf(p[i][e]) == INFINITY ? p[i][e] : fz * p[i][e]) : 0.f;
     }
   }
   const float inv = total == 0.f ? 0.f : 1.f / total;
