@@ -403,8 +403,10 @@ __global__ __launch_bounds__(64 * WR * WK, MINW) void k_attention_masked(AttnArg
     }
   }
   if (!odd) return;
+  // every seen score is -infinity: zeros, whatever the values hold (with splits the joining kernel knows)
+  const bool none = g.splits == 1 && total == 0.f;
   walk(std::integral_constant<int, COUNT>());
-  if (wk > 0 || !live) return;
+  if (wk > 0 || !live || none) return;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -456,10 +458,12 @@ __global__ __launch_bounds__(256) void k_attention_join(AttnArgs g) {
         o[e] += z0 + i < g.splits ? (fabsf(p[i][e]) == INFINITY ? p[i][e] : fz * p[i][e]) : 0.f;
     }
   }
-  const float inv = total == 0.f ? 0.f : 1.f / total;
+  const float inv = 1.f / total;
+#pragma unroll
+  for (int e = 0; e < E; ++e) o[e] = total == 0.f ? 0.f : o[e] * inv;          // zeros, also where an infinity was seen
   uint16_t* out = a.out + (int64_t)b * a.os[0] + (int64_t)qi * a.os[1] + (int64_t)qh * a.os[2] + lane * E;
-  if constexpr (E == 2) *reinterpret_cast<uint32_t*>(out) = f2bf2(o[0] * inv, o[1] * inv);
-  else *out = f2bf(o[0] * inv);
+  if constexpr (E == 2) *reinterpret_cast<uint32_t*>(out) = f2bf2(o[0], o[1]);
+  else *out = f2bf(o[0]);
 }
 
 template <int D, int WR, int WK, int KPW, int NST, int MINW>

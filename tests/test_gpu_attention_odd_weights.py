@@ -26,3 +26,25 @@ def test_an_infinite_value_of_next_to_no_weight_shows(d, h, hk, nq, nk, work):
         got, want = run(q, k, v2, work=work), clean.clone()
         want[:, :, h - h // hk:, 5] = value
         assert bool(((got == want) | (got.isnan() & want.isnan())).all()), (value, key)
+
+
+@pytest.mark.parametrize("d,h,hk,nq,nk", SHAPES)
+@pytest.mark.parametrize("work", [True, False])
+def test_scores_of_minus_infinity(d, h, hk, nq, nk, work):
+    # all of them: zeros, whatever the values hold; all but one key's: that key's value, and infinities that any seen key holds
+    log(f"{nq} over {nk}, {h} / {hk} heads of {d}, scratch {work}")
+    q, k, v = make(d + nk, 1, nq, nk, h, hk, d)
+    q.fill_(1.0)
+    k.fill_(float("-inf"))
+    assert bool((run(q, k, v, work=work) == 0).all())
+    v2 = v.clone()
+    for value, key in ((float("inf"), 3), (float("nan"), nk // 2), (float("-inf"), nk - 1)):
+        v2[0, key, hk - 1, 5] = value
+        assert bool((run(q, k, v2, work=work) == 0).all()), (value, key)
+    k[0, nk // 3] = 0.5
+    v2 = v.clone()
+    v2[0, 3, hk - 1, 5], v2[0, nk - 1, 0, 7] = float("inf"), float("-inf")
+    want = v[:, nk // 3].repeat_interleave(h // hk, dim=1)[:, None].expand(1, nq, h, d).clone()
+    assert bool((run(q, k, v, work=work) == want).all())
+    want[:, :, h - h // hk:, 5], want[:, :, :h // hk, 7] = float("inf"), float("-inf")
+    assert bool((run(q, k, v2, work=work) == want).all())
