@@ -97,7 +97,7 @@ typedef struct {
   int32_t batch, heads, kv_heads, head_dim, q_len, kv_len;
   int32_t causal;
   int32_t window_left, window_right, sinks;
-  float scale;               /* > 0; 0: 1 / sqrt(head_dim) */
+  float scale;               /* > 0, at most 2^127; 0: 1 / sqrt(head_dim) */
   void* work;
   uint64_t work_bytes;
 } tpo_attention_args;

@@ -106,7 +106,8 @@ tp_status tpo_attention(const tpo_attention_args* a, void* stream) {
   if (a->head_dim != 64 && a->head_dim != 128) return inval(who, "head_dim must be 64 or 128");
   if (a->causal != 0 && a->causal != 1) return inval(who, "causal must be 0 or 1");
   if (a->sinks < 0) return inval(who, "sinks < 0");
-  if (!(a->scale >= 0.f) || std::isinf(a->scale)) return inval(who, "scale must be finite and not negative");
+  // (the kernels multiply by scale log2(e), which has to be finite too)
+  if (!(a->scale >= 0.f) || a->scale > 0x1p127f) return inval(who, "scale must be at most 2^127 and not negative");
   if ((uintptr_t)a->work % 256) return inval(who, "work must be 256-byte aligned");
   if (a->batch == 0 || a->q_len == 0) return ok();
   if (!a->q || !a->out || (a->kv_len > 0 && (!a->k || !a->v))) return inval(who, "NULL buffer");
