@@ -7,11 +7,11 @@
 #include <chrono>
 #include <cstring>
 #include <new>
-#include <thread>
 
 #include <hip/hip_ext.h>
 
 #include "../core/errors.hpp"
+#include "../core/parts.hpp"
 #include "../core/w4.hpp"
 #include "../kernels/kernels.hpp"
 #include "../kernels/touch.hpp"
@@ -840,38 +840,32 @@ tp_status tp_register_model(tp_ctx* c, const tp_model_desc* desc, const void* ho
   if (nb > host_bytes) std::memset(static_cast<char*>(m->host) + host_bytes, 0, nb - host_bytes);
   if (m->spec.packed_mlp) {
     // weight matrices in the skinny-GEMM block order, one thread per group of layers
-    std::vector<std::thread> th;
     const int L = m->spec.dims[0], W = m->spec.dims[1];
-    const int nt = std::max(1, std::min(8, L));
-    for (int w = 0; w < nt; ++w)
-      th.emplace_back([&, w] {
-        for (int l = w; l < L; l += nt) {
-          const tp_tensor_desc& t = m->spec.t(l, TP_ROLE_W);
-          pack_rows16x128(reinterpret_cast<const uint16_t*>(static_cast<const char*>(host_weights) + t.offset),
-                          reinterpret_cast<uint16_t*>(static_cast<char*>(m->host) + t.offset), W, W);
-        }
-      });
-    for (auto& t : th) t.join();
+    const int nt = std::max(1, std::min(kMostParts, L));
+    in_parts(nt, [&](int w) {
+      for (int l = w; l < L; l += nt) {
+        const tp_tensor_desc& t = m->spec.t(l, TP_ROLE_W);
+        pack_rows16x128(reinterpret_cast<const uint16_t*>(static_cast<const char*>(host_weights) + t.offset),
+                        reinterpret_cast<uint16_t*>(static_cast<char*>(m->host) + t.offset), W, W);
+      }
+    });
   }
   if (m->spec.group) {
     // 4-bit matrices and their scales in blocked order (no padding: whole 16 rows and 128 columns), tensors by turns
-    std::vector<std::thread> th;
-    for (uint32_t w = 0; w < 8; ++w)
-      th.emplace_back([&, w] {
-        for (uint32_t i = w; i < m->spec.tensors.size(); i += 8) {
-          const tp_tensor_desc& t = m->spec.tensors[i];
-          const int32_t sr = scale_role(t.role);
-          if (sr < 0) continue;
-          const tp_tensor_desc& sc = m->spec.t(t.layer, (uint32_t)sr);
-          const char* src = static_cast<const char*>(host_weights);
-          char* dst = static_cast<char*>(m->host);
-          w4_pack_codes(reinterpret_cast<const uint8_t*>(src + t.offset), t.shape[0], t.shape[1],
-                        reinterpret_cast<uint8_t*>(dst + t.offset));
-          w4_pack_scales(reinterpret_cast<const uint16_t*>(src + sc.offset), t.shape[0], t.shape[1], m->spec.group,
-                         reinterpret_cast<uint16_t*>(dst + sc.offset));
-        }
-      });
-    for (auto& t : th) t.join();
+    in_parts(kMostParts, [&](int w) {
+      for (size_t i = w; i < m->spec.tensors.size(); i += kMostParts) {
+        const tp_tensor_desc& t = m->spec.tensors[i];
+        const int32_t sr = scale_role(t.role);
+        if (sr < 0) continue;
+        const tp_tensor_desc& sc = m->spec.t(t.layer, (uint32_t)sr);
+        const char* src = static_cast<const char*>(host_weights);
+        char* dst = static_cast<char*>(m->host);
+        w4_pack_codes(reinterpret_cast<const uint8_t*>(src + t.offset), t.shape[0], t.shape[1],
+                      reinterpret_cast<uint8_t*>(dst + t.offset));
+        w4_pack_scales(reinterpret_cast<const uint16_t*>(src + sc.offset), t.shape[0], t.shape[1], m->spec.group,
+                       reinterpret_cast<uint16_t*>(dst + sc.offset));
+      }
+    });
   }
   if (c->cfg.copy_method == TP_COPY_PAGEABLE) {
     m->pageable.reset(new (std::nothrow) char[nb]);
