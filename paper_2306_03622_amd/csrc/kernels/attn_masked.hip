@@ -21,8 +21,7 @@
 // row, which 0 would multiply, may hold infinities or NaN: those show as NaN in the sums, and a workgroup that finds
 // any such result at the end walks its keys twice more: once with what is not finite replaced by 0, and once counting,
 // for each row and column, the replaced values of seen keys, which then set the output.
-#include <algorithm>
-
+#include "attn_plan.hpp"
 #include "gemm_tile.hpp"
 
 namespace tp {
@@ -514,48 +513,21 @@ hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s) 
   const int64_t rows = (int64_t)a.q_len * g.share;
   // 32-bit offsets inside a tile of up to 128 keys
   if (rows * a.kv_heads * a.batch >= 1ll << 31 || a.ks[1] > 1 << 23 || a.vs[1] > 1 << 23) return hipErrorInvalidValue;
-  const int64_t heads = (int64_t)a.kv_heads * a.batch;
-  auto wgs = [&](int64_t r) { return (rows + r - 1) / r * heads; };      // workgroups of r rows
-  int64_t span = a.kv_len;                                               // keys that a workgroup walks, about
-  if (a.left >= 0 && (a.causal || a.right >= 0))
-    span = std::min<int64_t>(span, (int64_t)a.left + (a.causal ? 0 : a.right) + std::min<int64_t>(a.q_len, 128) + a.sinks);
-  // Splits of the keys over workgroups, to 256 of them, of at least three tiles of kt keys, as far as the scratch holds them (a
-  // lane of the joining wave for each). One token, 8 / 1 heads of 128 over 30,000 keys: 64 splits 17.9 us, 32 19.4, 16 25.2, none 240;
-  // 32 / 8 over 8000: 20 splits 16.2, 8 18.4; 8 x 32 / 8 over 3000: 8 splits 24.0, 16 27.7; ten over 600, 12 of 64: none 7.5, four 9.2.
-  auto split = [&](int64_t workgroups, int kt) {
-    const int64_t slots = rows * heads, fits = sp.partials ? (int64_t)(sp.partial_bytes / 4) / (slots * (a.dim + 2)) : 0;
-    g.splits = (int)std::max<int64_t>(1, std::min<int64_t>({256 / workgroups, span / (3 * kt), 64, fits}));
-    g.part = sp.partials;
-  };
-  // Measured on MI355X (us), heads / key/value heads x dim, queries over keys:
-  //   32 rows, four waves deep: few tokens, whose cost is the latency, and short sequences that would not give every CU a larger tile:
-  //     32 / 8 x 128, 8 over 8000 24.5 (64 rows 28.1), 20 over 8000 22.6 (128 rows 31.1), 8 / 1, 1 over 30,000 29.4 (64
-  //     rows 31.7); 12 x 64, 5 x 96 5.3 (5.6), 512 over 512 7.4 (12.6).
-  //   64 rows, two deep, one tile more under way: tokens whose cost is the memory's: 32 / 8 x 128, 1 over 100,001 92.6 (32 rows 97.3), 16 x 1
-  //     with a window of 1024 19.9 (21.1); 12 x 64, 16 x 1 over 3000 36.6 (42.7). Also 32 / 8 x 128, 500 over 500 13.0 (128 rows, two
-  //     deep 22.1); at dim 64 up to four on every CU: 12 x 64, 8 x 512 16.9 (128 rows 18.2), 4096 with a window of 256 19.0 (22.6).
-  //   128 rows, two deep, 64 keys a wave, at dim 128 up to one on every CU: 32 / 8, 2 x 500 over 6000 with a window of 1024 30.8 (one deep
-  //     34.4), 100 over 5000 24.8 (29.0). But 32 / 32, 2 x 1000 53.1 (one deep 44.3).
-  //   256 rows for long walks at dim 128, two on every CU and more: 32 / 8, 4096 causal 150 (128 rows 158), 8191 552 (559).
-  //   128 rows else: 32 / 8 x 128, 4 x 2000 with a window of 512 99 (256 rows 110); 12 x 64, 8 x 2048 with
-  //     a window of 128 34.5 (64 rows 45). There 32 keys a wave, but 64 on long walks: 8000 causal 153 (32 keys 168), 4 x 2048 78 (85);
-  //     with the window 36.
-  const bool d64 = a.dim == 64, heavy = heads * span * a.dim >= 1 << 24;
-  if ((rows <= (d64 ? 64 : 128) && !heavy) || (rows > 64 && wgs(32) <= 256 && span <= 1024)) {
-    split(wgs(32), 128);
-    return d64 ? go<64, 1, 4, 1, 2, 2>(g, s) : go<128, 1, 4, 1, 2, 1>(g, s);
+  const int64_t span = attn_span(a.q_len, a.kv_len, a.causal, a.left, a.right, a.sinks);
+  const AttnPlan plan = attn_plan(a.dim, rows, (int64_t)a.kv_heads * a.batch, span, sp.partials ? sp.partial_bytes : 0);
+  g.splits = plan.splits;
+  g.part = sp.partials;
+  switch (plan.variant) {     // dim, waves over rows and keys, 32-key blocks a wave, stages, least waves per SIMD
+    case ATTN64_R32: return go<64, 1, 4, 1, 2, 2>(g, s);
+    case ATTN64_R64: return go<64, 2, 2, 1, 3, 2>(g, s);
+    case ATTN64_R128: return go<64, 4, 1, 1, 3, 2>(g, s);
+    case ATTN64_R128_LONG: return go<64, 4, 1, 2, 2, 2>(g, s);
+    case ATTN128_R32: return go<128, 1, 4, 1, 2, 1>(g, s);
+    case ATTN128_R64: return go<128, 2, 2, 1, 3, 1>(g, s);
+    case ATTN128_R128_DEEP: return go<128, 4, 2, 2, 2, 2>(g, s);
+    case ATTN128_R128: return go<128, 4, 1, 2, 2, 2>(g, s);
+    default: return go<128, 8, 1, 2, 2, 2>(g, s);
   }
-  if (rows <= 64 || (d64 ? wgs(64) <= 1024 : wgs(64) <= 256 && span <= 1024)) {
-    split(wgs(64), 64);
-    return d64 ? go<64, 2, 2, 1, 3, 2>(g, s) : go<128, 2, 2, 1, 3, 1>(g, s);
-  }
-  if (!d64 && wgs(128) <= 256) {
-    split(wgs(128), 128);
-    return go<128, 4, 2, 2, 2, 2>(g, s);
-  }
-  g.splits = 1;
-  if (d64) return span >= 1024 ? go<64, 4, 1, 2, 2, 2>(g, s) : go<64, 4, 1, 1, 3, 2>(g, s);
-  return span >= 2048 && wgs(256) >= 512 ? go<128, 8, 1, 2, 2, 2>(g, s) : go<128, 4, 1, 2, 2, 2>(g, s);
 }
 
 }  // namespace k
