@@ -63,6 +63,14 @@ def test_every_plan_can_be_launched(plan):
             assert up(m, bm) * up(n, bn) * threads < 2 ** 32, (m, n, k, g, p)
 
 
+def test_the_gpu_shapes_reach_every_kernel_with_every_group(plan):
+    from tests.test_gpu_linear_w4 import SHAPES
+    from tests.test_gpu_linear_w4_variants import SHAPES as MORE
+    shapes = [*SHAPES, *MORE]
+    variants, plans = plan(shapes)
+    assert {(p, s[3]) for s, p in zip(shapes, plans)} == {(p, g) for p in range(len(variants)) for g in (32, 64, 128)}
+
+
 @pytest.mark.parametrize("m,n", [(2 ** 30 - 127, 1), (2 ** 31 - 1, 1), (2 ** 31 - 1, 2 ** 24), (2 ** 14, 2 ** 24), (2 ** 29, 257)])
 def test_more_outputs_are_refused(m, n):
     a = linear_args(M=m, N=n, ldy=n)     # (addresses that are never read: refused before a launch)
