@@ -55,7 +55,8 @@ TP_API tp_status tpo_w4_quantize(const float* w, int32_t N, int32_t K, int32_t g
  * and sums are exact bf16 products in fp32 sums, scales applied to each group's sum, one rounding at the end.
  * x starts at a 16-byte boundary and ldx is a multiple of 8 below 2^23; wq and scales start at 16-byte boundaries. y may
  * be res (same ldr and ldy, both bf16); apart from that outputs do not overlap inputs. M = 0 does nothing. M in whole 128s
- * times N in whole 256s is below 2^38. An infinite x[m][k] makes row m NaN. */
+ * times N in whole 256s is below 2^38. An infinite or NaN x[m][k] makes row m NaN, whatever the activation; finite inputs of
+ * which 31 times a group's sum of |x| reaches 2^128 may overflow. */
 typedef struct {
   const void* x;
   int64_t ldx;
@@ -80,9 +81,12 @@ TP_API tp_status tpo_linear_w4(const tpo_linear_w4_args* a, void* stream);
  * sequence; values are clamped to [0, q_len] and [0, kv_len]). Query i stands at p = kv_lens[b] - q_lens[b] + i, and sees
  * key j < kv_lens[b] if
  *   (causal: j <= p) and (j < sinks, or p - window_left <= j <= p + window_right; a negative bound is none).
- * out = sum over the seen j of softmax_j(scale q k_j) v_j, softmax in fp32; a query that sees no key (or whose
+ * out = sum over the seen j of softmax_j(scale q k_j) v_j; a query that sees no key (or whose
  * scores are all -infinity) gives zeros. Keys that a query does not see do not touch it, whatever they hold. Rows
- * i >= q_lens[b] of out are left as they are.
+ * i >= q_lens[b] of out are left as they are. Scores, exponentials and sums are fp32; each exponential is rounded to bf16
+ * before it multiplies v_j (not in the sum that divides), the result once more: off by 2^-8 of sum softmax_j |v_j| and 2^-8 of
+ * itself at most. Values of which 2^8 times a query's sum reaches 2^128 may overflow. An infinity or NaN in a seen v_j shows in its
+ * column, however little it weighs.
  * q and out: heads of head_dim (64 or 128) bf16 values; k and v: kv_heads, of which each serves heads / kv_heads
  * consecutive query heads. Strides in elements between sequences, tokens and heads ([0], [1], [2]); the values of a
  * head are contiguous. Every head's values start at a 16-byte boundary (strides are multiples of 8; k's and v's between tokens at most 2^23). A stride of 0

@@ -10,9 +10,10 @@
 //
 // Scores are computed transposed, S^T = K Q^T: lane l holds row l % 32 against keys 8 (i / 4) + 4 (l / 32) + i % 4 in
 // register i, so a row's maximum and sum stay in a lane and its partner l ^ 32. The output is transposed too, O^T =
-// V^T P^T: the exponentials, rounded to bf16 (as the matrix cores take them; the sum that divides
-// them is of the unrounded ones), are the B operand from the very registers they are in, V^T is read with the transposing
-// LDS load, and a row's rescaling is one factor per lane. The reference that exponents are taken from follows the maximum only
+// V^T P^T: the exponentials are the B operand from the very registers they are in, V^T is read with the transposing
+// LDS load, and a row's rescaling is one factor per lane. For that the exponentials are rounded to bf16, as the matrix cores
+// take V: a result is off by at most 2^-8 of the weights' mean of |v| for it, as much as its own rounding may add, and two
+// bf16 parts of each would double V's products. The sum that divides is of the unrounded ones. The reference that exponents are taken from follows the maximum only
 // when that has risen by 8 (a factor of 256, harmless in fp32 sums and in bf16, whose precision is relative).
 //
 // A key is seen if it lies in [lo, hi] (window and order) or in front of sk (sinks), three numbers per row. Only

@@ -139,10 +139,11 @@ __device__ __forceinline__ void w4_block(const uint4 (&xf)[MB][4], const uint4 (
 // a wave's run, the rows or the columns go out of their buffer's bounds, which reads zeros and moves nothing, so nothing
 // in the loop is conditional.
 //
-// Bound by the weights' way from HBM where there are many (1 x 32768 x 8192, 138 MB: 30 us, 4.6 TB/s, the card's copy rate being 4.95),
-// else by the chain of one launch, a load and a reduction: 1 x 768 x 768 3.0 us (an empty launch takes about as much), 8 x
-// 4096 x 4096 5.9 us, of which each workgroup's reading of the same activations through its L2 is the larger part. Waves
-// split the columns, not the rows, so that the loads of a few hundred workgroups cover the latency.
+// Bound by the weights' way from HBM where there are many (1 x 32768 x 8192, 138 MB: 30 to 33 us, 4.2 to 4.6 TB/s, where a read
+// alone reaches 6.1), else by the chain of a launch, the loads' round trips and a reduction: 1 x 768 x 768 3.0 us (an empty
+// launch takes about as much); 8 x 4096 x 4096 5.9 us, eight k-blocks a wave, two in flight: four turns, matrix instructions in 8% of the
+// time and vector ones in 15%; 100 x 1000 x 2048 5.9, both k-blocks of a wave in flight. Waves split the columns, not the rows, so that the
+// loads of a few hundred workgroups cover the latency.
 template <int MT, int NB, int NW, int GP, int U>
 __global__ __launch_bounds__(NW * 64) void k_w4_rows(W4Args g) {
   const LinearW4& a = g.a;
@@ -220,11 +221,12 @@ __global__ __launch_bounds__(NW * 64) void k_w4_rows(W4Args g) {
 // while the weight blocks pass: one is unpacked once, multiplied with all MB fragments, and its scale applied to the
 // finished group.
 //
-// Bound, for the largest tiles, by issue slots and the LDS: 8192 x 4096 x 4096 in groups of 128 takes 304 us, 0.90 PFLOP/s
-// (a plain bf16 product of that size by the library 214 us), the matrix cores busy 45% of the time; beside 80 matrix
-// instructions a wave issues about 200 others a stage, and all waves read their fragments together behind the barrier. Neither
-// waves of 32 rows x 128 outputs (11% slower), nor activation sums shared between waves (2%), nor fragments read half a
-// stage ahead gained anything. Mid sizes are chains of few stages: 1024 x 2304 x 768 12.1 us, 100 x 1000 x 2048 6.0.
+// Bound, for the largest tiles, by matrix and vector instructions that hardly overlap: 8192 x 4096 x 4096 in groups of 128
+// takes 302 us, 0.91 PFLOP/s (a plain bf16 product of that size by the library 214 us). Beside 80 matrix instructions (16 cycles each) a
+// wave issues about 275 vector ones (4 each) a stage; the matrix pipes are busy 47% of the time, the vector ones 41%, and the two waves of a
+// SIMD leave the same barrier together. Neither waves of 32 rows x 128 outputs (11% slower), nor activation sums shared between
+// waves (2%), nor fragments read half a stage ahead gained anything. Mid sizes are chains of few stages: 1024 x 2304 x 768 12.1 us, six
+// stages on 576 workgroups, of which 64 CUs hold three and the others two.
 template <int BN, int BM, int WGN, int WGM, int KS, int NST, int GP>
 struct W4Tile {
   static constexpr int NW = WGN * WGM, NB = BN / WGN / 16, MB = BM / WGM / 16;

@@ -18,10 +18,12 @@ enum { W4_ROWS16, W4_ROWS32, W4_ROWS64, W4_TILE32X32, W4_TILE64X32, W4_TILE64X32
 
 // Fitted to 2499 passes on MI355X (13 shapes from 96 x 200 to 8192 x 32768, the three groups, 1 to 5000 rows, graph replay,
 // operands rotating beyond the L2s): choosing by the model costs 3% over the best variant of each case on average.
-// What they trade, us: 4096 x 4096, groups of 128: 1 row ROWS16 4.8, ROWS64 8; 32 rows ROWS32 8.5, ROWS16 11.4; 64 rows
-// ROWS64 9.5, ROWS32 13; 128 rows TILE64X32_DEEP 12.9, ROWS64 16; 256 rows TILE64X64 22.5, TILE64X32_DEEP 25; 1024 rows
-// TILE128X64_WIDE 49.8, TILE64X64 58; 2048 rows TILE256X128 80, TILE128X64_WIDE 90; 8192 rows 295, 351. 768 x 4096: 24 rows ROWS16 5.1,
-// 80 rows TILE64X32 6.1.
+// What they trade, us, in groups of 128, of 4096 outputs and columns: 1 row ROWS16 4.9, ROWS64 7.9; 32 rows ROWS32 8.3, ROWS16 11.6;
+// 64 rows ROWS64 9.7, ROWS32 13.9; 128 rows TILE64X32_DEEP 12.7, ROWS64 16.5; 256 rows TILE64X64 23.2, TILE64X32_DEEP 23.1 and 24.3;
+// 1024 rows TILE128X64_WIDE 51.5, TILE64X64 61.9; 2048 rows TILE256X128 79, TILE128X64_WIDE 95 (in groups of 32 99 and 116); 8192 rows
+// 312, 355. Of 4096 outputs and 768 columns: 24 rows ROWS16 4.2, ROWS32 4.4; 80 rows TILE64X32 5.3, ROWS64 6.2, TILE32X32 8.1. Of 768
+// outputs and 4096 columns: 24 rows ROWS16 7.1, ROWS32 7.7, TILE32X32 8.7. The model counts rounds of 256 workgroups, though a CU holds
+// up to three of the smaller tiles at a time: it expects 15.0 of 1024 x 2304 x 768, which takes 12.
 constexpr W4Variant kW4[W4_VARIANTS] = {
     {16, 16, 4, 256, 2.565, 0.076, 0.0, 0.434, 0.055},    {32, 16, 8, 512, 2.405, 0.987, 0.0, 1.042, 0.069},
     {64, 16, 8, 512, 2.186, 0.465, 0.0, 1.445, 0.171},    {32, 32, 4, 512, 1.345, 2.383, 0.0, 0.689, 0.026},
@@ -51,7 +53,7 @@ inline int w4_plan(int64_t M, int64_t N, int64_t K, int group) {
   for (int i = 0; i < W4_VARIANTS; ++i) {
     if (!w4_fits(i, M, N)) continue;
     // the largest tiles only where 16 k-blocks and more make up for the ring's filling, as the model does not see
-    // (5000 rows, 1024 x 256: 20.4 us, TILE128X64 14.9), or where no others can be launched
+    // (5000 rows, 1024 outputs, 256 columns: 16.0 us, TILE128X64 12.1), or where no others can be launched
     if (i == W4_TILE256X128 && K < 16 * 128 && best >= 0) continue;
     const double t = w4_us(kW4[i], M, N, K, group);
     if (best < 0 || t < us) {
