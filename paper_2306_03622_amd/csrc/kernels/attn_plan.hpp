@@ -30,7 +30,8 @@ inline AttnPlan attn_plan(int dim, int64_t rows, int64_t heads, int64_t span, ui
   // Splits of the keys over workgroups, to 256 of them, of at least three tiles of kt keys, as far as the scratch holds them (a
   // lane of the joining wave for each). One token, 8 / 1 heads of 128 over 30,000 keys: 64 splits 18.7 us, 32 19.9, 16 25.4, none 241;
   // 32 / 8 over 8000: 20 splits 16.8, 8 18.7; 8 x 32 / 8 over 3000: four splits 24.8, two 31.9, eight 28.5; ten over 600, 12 of 64: none
-  // 7.6, four 8.8. From 129 workgroups on there is one walk for each, so that up to 511 some CUs have more to do than others.
+  // 7.6, four 8.8. From 129 workgroups on there is one walk for each, so that up to 511 some
+  // CUs have more to do than others: one token of 16 / 17 / 32 / 33 sequences, 32 / 8 over 4096, 55 / 69 / 97 / 149.
   auto splits = [&](int64_t workgroups, int kt) {
     const int64_t fits = (int64_t)(scratch / 4) / (rows * heads * (dim + 2));
     return (int)std::max<int64_t>(1, std::min<int64_t>({256 / workgroups, span / (3 * kt), 64, fits}));
