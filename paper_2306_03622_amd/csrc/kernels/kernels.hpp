@@ -132,6 +132,63 @@ struct Attention {
 };
 hipError_t attention_masked(const Attention& a, const Split& sp, hipStream_t s);
 
+// A paged key/value cache (torpor_serve.h, whose argument block it mirrors).
+struct Cache {
+  void *k = nullptr, *v = nullptr;
+  uint8_t* exps = nullptr;          // e4m3 only
+  int64_t ks[3] = {}, vs[3] = {};   // bytes between pages, tokens, heads
+  int e4m3 = 0;
+  int pages = 0, lg = 0, heads = 0, dim = 0;        // lg: log2 of the page size
+};
+
+// The pages and lengths of a call's sequences.
+struct Pages {
+  const int32_t* table = nullptr;
+  int64_t table_stride = 0;
+  const int32_t *q_lens = nullptr, *kv_lens = nullptr;
+  int batch = 0, q_len = 0, max_pages = 0;
+};
+
+// Rows of keys and values into the cache (append) or out of it; strides in elements, as there.
+struct CacheRows {
+  Cache c;
+  Pages p;
+  uint16_t *k = nullptr, *v = nullptr;
+  int64_t rks[3] = {}, rvs[3] = {};
+};
+hipError_t cache_append(const CacheRows& a, hipStream_t s);
+hipError_t cache_read(const CacheRows& a, hipStream_t s);
+
+struct CacheAttention {
+  Cache c;
+  Pages p;
+  const uint16_t* q = nullptr;
+  uint16_t* out = nullptr;
+  int64_t qs[3] = {}, os[3] = {};
+  int heads = 0, kv_len = 0;
+  int window = -1, sinks = 0;
+  float scale = 0.f;
+};
+hipError_t cache_attention(const CacheAttention& a, const Split& sp, hipStream_t s);
+
+// Low-rank adapters (torpor_serve.h): y = act(base + scale B A x), the adapter by row.
+struct Lora {
+  const uint16_t* x = nullptr;
+  int64_t ldx = 0;
+  const uint16_t *a = nullptr, *b = nullptr;
+  int64_t as = 0, bs = 0;           // elements between adapters
+  const int32_t *adapter = nullptr, *ranks = nullptr;
+  const float* scales = nullptr;
+  const void* base = nullptr;
+  int64_t ldbase = 0;
+  void* y = nullptr;
+  int64_t ldy = 0;
+  int f32 = 0;                      // base and y
+  int M = 0, N = 0, K = 0, R = 0, adapters = 0;
+  int act = 0;                      // ACT_*
+};
+hipError_t lora(const Lora& a, const Split& sp, hipStream_t s);
+
 // lens[b] = the number of ids of row b in front of its first negative one; ids [B][S].
 hipError_t seq_lengths(const int32_t* ids, int B, int S, int32_t* lens, hipStream_t s);
 
