@@ -8,8 +8,8 @@
 // Without scratch k_lora does both in one launch and computes t anew for every 256 outputs.
 //
 // t is taken as bf16 parts (two, three for fp32 results: 2^-16 and 2^-24 of t), all multiplied by B, whose values are bf16 as they are.
-// Operands: A's rows r against x's rows m (t^T), then B's rows n against t's rows m (y^T), rows n of four blocks interleaved so
-// that a lane ends with 16 consecutive outputs of its row. What lies behind a rank is not used, whatever it holds.
+// Operands: A's rows r against x's rows m (t^T), then t's rows m against B's rows n, those of four blocks interleaved so
+// that a lane ends with four consecutive outputs of a row. What lies behind a rank is not used, whatever it holds.
 #include "lora_plan.hpp"
 #include "serve_args.hpp"
 
@@ -22,7 +22,8 @@ struct LoraArgs {
   int splits;             // over K
   int slots;              // workgroups (or waves) that share a tile's adapters
   int tiles_n;            // blocks of outputs
-  int vec;                // base and y in whole 16 bytes
+  int vec;                // base and y four outputs at a time
+  int run, xcds;          // second product: blocks of 64 outputs a workgroup, XCDs that tiles are handed to
 };
 
 template <>
@@ -56,54 +57,53 @@ __device__ __forceinline__ int rank_of(const Lora& a, int ad) { return a.ranks ?
 // The rest of t behind its bf16 part (none behind an infinity or NaN).
 __device__ __forceinline__ float rest_of(float t, uint16_t part) { return fabsf(t) < INFINITY ? t - bf2f(part) : 0.f; }
 
-// 16 outputs of row m from n on: base, activation, rounding.
+// Four outputs of a row from n on: the base's values, loaded ahead where they come in one piece, and the rest.
 template <bool F32>
-__device__ __forceinline__ void finish(const Lora& a, bool vec, int m, int n, const f32x4 (&acc)[4]) {
-  if (n >= a.N) return;
-  if (vec && n + 16 <= a.N) {
+struct Run {
+  uint4 w;                // fp32, or bf16 pairs in x and y
+  // (m: a row that is there, n: any output; what is not stored is not used)
+  __device__ __forceinline__ void load(const Lora& a, bool vec, int64_t m, int n) {
+    w = zeros();
+    if (!a.base || !vec || n + 4 > a.N) return;
+    const char* p = static_cast<const char*>(a.base) + (m * a.ldbase + n) * (F32 ? 4 : 2);
     if constexpr (F32) {
-      const float* bp = static_cast<const float*>(a.base) + m * a.ldbase + n;
-      float* yp = static_cast<float*>(a.y) + m * a.ldy + n;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f32x4 v = acc[e];
-        if (a.base) v += *reinterpret_cast<const f32x4*>(bp + 4 * e);
+      w = load16(p);
+    } else {
+      const uint2 u = *reinterpret_cast<const uint2*>(p);
+      w.x = u.x, w.y = u.y;
+    }
+  }
+  // base + v, activation, rounding
+  __device__ __forceinline__ void finish(const Lora& a, bool vec, int64_t m, int n, f32x4 v) const {
+    if (n >= a.N) return;
+    if (vec && n + 4 <= a.N) {
+      char* p = static_cast<char*>(a.y) + (m * a.ldy + n) * (F32 ? 4 : 2);
+      if constexpr (F32) {
+        v += __builtin_bit_cast(f32x4, w);
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = lora_act(v[i], a.act);
-        *reinterpret_cast<f32x4*>(yp + 4 * e) = v;
+        *reinterpret_cast<f32x4*>(p) = v;
+      } else {
+        v += f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = lora_act(v[i], a.act);
+        *reinterpret_cast<uint2*>(p) = make_uint2(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]));
       }
-    } else {
-      const uint16_t* bp = static_cast<const uint16_t*>(a.base) + m * a.ldbase + n;
-      uint16_t* yp = static_cast<uint16_t*>(a.y) + m * a.ldy + n;
+      return;
+    }
 #pragma unroll
-      for (int e = 0; e < 4; e += 2) {
-        uint4 w = zeros();
-        if (a.base) w = load16(bp + 4 * e);
-        uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float lo = lora_act(acc[e + j / 2][2 * (j % 2)] + __uint_as_float(u[j] << 16), a.act);
-          const float hi = lora_act(acc[e + j / 2][2 * (j % 2) + 1] + __uint_as_float(u[j] & 0xffff0000u), a.act);
-          u[j] = f2bf2(lo, hi);
-        }
-        *reinterpret_cast<uint4*>(yp + 4 * e) = make_uint4(u[0], u[1], u[2], u[3]);
+    for (int j = 0; j < 4; ++j) {
+      if (n + j >= a.N) continue;
+      if constexpr (F32) {
+        const float base = a.base ? static_cast<const float*>(a.base)[m * a.ldbase + n + j] : 0.f;
+        static_cast<float*>(a.y)[m * a.ldy + n + j] = lora_act(v[j] + base, a.act);
+      } else {
+        const float base = a.base ? bf2f(static_cast<const uint16_t*>(a.base)[m * a.ldbase + n + j]) : 0.f;
+        static_cast<uint16_t*>(a.y)[m * a.ldy + n + j] = f2bf(lora_act(v[j] + base, a.act));
       }
     }
-    return;
   }
-#pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    if (n + j >= a.N) continue;
-    float v = acc[j / 4][j % 4];
-    if constexpr (F32) {
-      if (a.base) v += static_cast<const float*>(a.base)[m * a.ldbase + n + j];
-      static_cast<float*>(a.y)[m * a.ldy + n + j] = lora_act(v, a.act);
-    } else {
-      if (a.base) v += bf2f(static_cast<const uint16_t*>(a.base)[m * a.ldbase + n + j]);
-      static_cast<uint16_t*>(a.y)[m * a.ldy + n + j] = f2bf(lora_act(v, a.act));
-    }
-  }
-}
+};
 
 // The adapter of row m0 + lane (lanes below ROWS), -1: none.
 template <int ROWS>
@@ -119,34 +119,56 @@ __device__ __forceinline__ int nth_of(unsigned long long mask, int lane) {
   return __builtin_amdgcn_ds_permute((mask >> lane & 1 ? before : 63) * 4, mask >> lane & 1 ? lane : 0);
 }
 
-// t[z][m][r] of the rows of 32 that name an adapter of this slot: the waves side by side along k in steps of 32, joined in LDS in
-// wave order. RB: blocks of 16 ranks.
-template <int RB, int W>
+// Workgroups are handed out to the eight XCDs in turn: tiles side by side, whose rows often have the same adapter, for one XCD.
+__device__ __forceinline__ int tile_of(int id, int tiles) {
+  const int each = tiles >> 3, more = tiles & 7, x = id & 7;
+  return id >= each * 8 + more ? id : x * each + min(x, more) + (id >> 3);
+}
+
+// 16 bytes per lane straight into LDS: lane l's land at `dst` + 16 l. (m0 is set in the block, which holds the wait state behind it.)
+__device__ __forceinline__ void lane_to_lds(const void* p, uint32_t dst) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(p) : "m0");
+}
+__device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void vm_left() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
+
+// t[z][m][r] of the rows of 32 that name an adapter of this slot. The waves take steps of 64 k (a cache line of each row of x and A) in
+// turns, each through a ring of NST steps in LDS of its own, and join in wave order. The operands' lanes lie row by row, 16 bytes of
+// each: loaded so, a load takes 64 cycles of the address path (measured 15 bytes a cycle and CU, 42 us for 8192 rows of 4096, rank 64);
+// into LDS eight lanes bring a row's line. Its eight chunks are moved by key_of(row) so that 16 rows' same chunk falls on different banks.
+// RB: blocks of 16 ranks.
+__device__ __forceinline__ int key_of(int row) { return row >> 1 & 7; }
+
+template <int RB, int W, int NST>
 __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
-  __shared__ float part[W][16][33];
+  constexpr int STAGE = 16 * (2 + RB) * 128, RING = NST * STAGE, JOIN = W * 16 * 33 * 4, LDS = W * RING > JOIN ? W * RING : JOIN;
+  static_assert(LDS <= 160 * 1024, "LDS");
+  __shared__ __attribute__((aligned(1024))) char lds[LDS];
   const Lora& a = g.a;
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int at = blockIdx.x;
   const int z = at % g.splits;
   at /= g.splits;
-  const int slot = at % g.slots, m0 = at / g.slots * 32;
+  // slots last: the others' workgroups may have nothing to do
+  const int tiles = (a.M + 31) / 32, slot = at / tiles, m0 = tile_of(at % tiles, tiles) * 32;
   const int mine = adapter_at<32>(a, m0, lane);
-  const int full = a.K >> 5, stride = g.splits * W;
+  const int full = a.K >> 6, stride = g.splits * W, s0 = z * W + wave, n = full > s0 ? (full - s0 + stride - 1) / stride : 0;
+  const char* ring = lds + wave * RING;
+  const uint32_t ring0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * RING;
 
   auto body = [&](auto blocks, int ad, int rows, int count) __attribute__((always_inline)) {
-    constexpr int MB = decltype(blocks)::value;
+    constexpr int MB = decltype(blocks)::value, LPS = 2 * (MB + RB);
     const int rank = rank_of(a, ad);
-    int m[MB];
-    const uint16_t *x[MB], *down[RB];
+    const uint16_t *xa = a.a + ad * a.as;
+    const uint16_t* from[LPS];                      // this lane's rows: x's (behind the last the first again, not written), A's
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      const int j = mb * 16 + r16;
-      m[mb] = m0 + __shfl(rows, j < count ? j : 0, 64);         // behind the last: the first again, not written
-      x[mb] = a.x + m[mb] * a.ldx + 8 * q4;
+    for (int i = 0; i < LPS; ++i) {
+      const int r = 8 * i + (lane >> 3), j = r - 16 * MB, ch = (lane & 7) ^ key_of(r);
+      const int row = m0 + __shfl(rows, i < 2 * MB && r < count ? r : 0, 64);
+      from[i] = (i < 2 * MB ? a.x + row * a.ldx : xa + (int64_t)min(j, a.R - 1) * a.K) + 8 * ch;
     }
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) down[rb] = a.a + ad * a.as + (int64_t)min(rb * 16 + r16, a.R - 1) * a.K + 8 * q4;
     f32x4 d[RB][MB];
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb)
@@ -159,32 +181,56 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
         for (int mb = 0; mb < MB; ++mb)
           d[rb][mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(af[rb]), as_bf16x8(xf[mb]), d[rb][mb], 0, 0, 0);
     };
-    int s = z * W + wave;
-    constexpr int U = RB > 4 ? 2 : 4;               // steps loaded together
-    for (; s + (U - 1) * stride < full; s += U * stride) {
-      uint4 xf[U][MB], af[U][RB];
+    auto issue = [&](int at, int i) __attribute__((always_inline)) {
+      const int64_t k = (int64_t)(s0 + i * stride) * 64;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = (s + u * stride) * 32;
+      for (int l = 0; l < LPS; ++l) lane_to_lds(from[l] + k, ring0 + at * STAGE + l * 1024);
+    };
+    lds_reads_done();                               // (of the join before)
+    vm_left<0>();
 #pragma unroll
-        for (int mb = 0; mb < MB; ++mb) xf[u][mb] = load16(x[mb] + k);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) af[u][rb] = load16(down[rb] + k);
+    for (int i = 0; i < NST - 1; ++i)
+      if (i < n) issue(i, i);
+    int at = 0;
+    for (int i = 0; i < n; ++i) {
+      lds_reads_done();
+      if (i + NST - 1 < n) {
+        issue(at == 0 ? NST - 1 : at - 1, i + NST - 1);
+        vm_left<(NST - 1) * LPS>();
+      } else {
+        vm_left<0>();
       }
+      const char* base = ring + at * STAGE;
 #pragma unroll
-      for (int u = 0; u < U; ++u) multiply(xf[u], af[u]);
+      for (int u = 0; u < 2; ++u) {
+        auto frag = [&](int block) { return load16(base + (block * 16 + r16) * 128 + (((4 * u + q4) ^ key_of(r16)) << 4)); };
+        uint4 xf[MB], af[RB];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb) xf[mb] = frag(mb);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) af[rb] = frag(MB + rb);
+        multiply(xf, af);
+      }
+      at = at + 1 == NST ? 0 : at + 1;
     }
-    for (; s * 32 < a.K; s += stride) {
-      const int k = s * 32;
-      const bool in = k + 8 * q4 < a.K;             // K is a multiple of 8
-      uint4 xf[MB], af[RB];
+    if (a.K & 63 && s0 % stride == full % stride) {   // the last columns, no whole step
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb) xf[mb] = in ? load16(x[mb] + k) : zeros();
+      for (int u = 0; u < 2; ++u) {
+        const int k = full * 64 + 32 * u + 8 * q4;
+        const bool in = k < a.K;                    // K is a multiple of 8
+        uint4 xf[MB], af[RB];
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) af[rb] = in ? load16(down[rb] + k) : zeros();
-      multiply(xf, af);
+        for (int mb = 0; mb < MB; ++mb) {
+          const int j = mb * 16 + r16, row = m0 + __shfl(rows, j < count ? j : 0, 64);
+          xf[mb] = in ? load16(a.x + row * a.ldx + k) : zeros();
+        }
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) af[rb] = in ? load16(xa + (int64_t)min(rb * 16 + r16, a.R - 1) * a.K + k) : zeros();
+        multiply(xf, af);
+      }
     }
     const float scale = a.scales ? a.scales[ad] : 1.f;
+    float(*part)[16][33] = reinterpret_cast<float(*)[16][33]>(lds);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       __syncthreads();                              // (what was there has been read)
@@ -202,6 +248,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
         if (j < count && r < a.R) g.t[((int64_t)z * a.M + m0 + row) * a.R + r] = r < rank ? t * scale : 0.f;
       }
     }
+    __syncthreads();
   };
   unsigned long long left = __ballot(mine >= 0);
   for (int j = 0; left; ++j) {
@@ -215,56 +262,88 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
   }
 }
 
-// y of the rows of 64 that name an adapter of this slot (slot 0: those without one too), 64 outputs a wave. RC: chunks of 32 ranks.
+// y of the rows of 64 that name an adapter of this slot (and in slot 0 those without one), g.run blocks of 64 outputs. The rows of one
+// adapter go to the waves, 16 to each; the parts of t stay in registers. A block of B (64 rows, in memory as they lie) goes through
+// registers into LDS, two blocks in turn, so that the next one's values and base are under way while one is computed. Output n
+// = 64 nb + 4 l + e comes from lane l and block e: a lane has four consecutive outputs of four rows, 16 lanes a row's 64. In
+// LDS row 16 e + l holds B's row 4 l + e, its chunks moved by at_of so that 16 rows' same chunk falls on different banks.
 template <bool F32, int RC>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
-  constexpr int PARTS = F32 ? 3 : 2;
+  constexpr int W = 4, PARTS = F32 ? 3 : 2, ROWS = 16 * W, PITCH = 64 * RC, CPR = 4 * RC, MINE = CPR / W;
+  __shared__ __attribute__((aligned(16))) char lds[2][64 * PITCH];
   const Lora& a = g.a;
-  const int lane = threadIdx.x & 63, r16 = lane & 15, q4 = lane >> 4;
-  int at = blockIdx.x;
-  const int n0 = (at % g.tiles_n * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 64;
-  at /= g.tiles_n;
-  const int slot = at % g.slots, m0 = at / g.slots * 64;
-  if (n0 >= a.N) return;
-  const int mine = adapter_at<64>(a, m0, lane);
+  const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  // Workgroups are handed out to the eight XCDs in turn: a tile's outputs all go to one of them, so that its L2 cache sees whole
+  // rows, not the same few columns (a few of its channels) of all rows. Slots last: the others' may have nothing to do.
+  const int tiles = (a.M + ROWS - 1) / ROWS, xcds = g.xcds, each = (tiles + xcds - 1) / xcds, id = blockIdx.x;
+  const int part = id / xcds % g.tiles_n, job = id / xcds / g.tiles_n, slot = job / each, tile = id % xcds * each + job % each;
+  if (tile >= tiles) return;
+  const int m0 = tile * ROWS, nb0 = part * g.run, nb1 = min(nb0 + g.run, (a.N + 63) / 64);
+  auto at_of = [](int row, int ch) { return row * PITCH + ((ch ^ (RC == 1 ? row >> 2 & 3 : RC == 2 ? row >> 1 & 7 : row & 15)) << 4); };
+  const int mine = adapter_at<ROWS>(a, m0, lane);
 
-  auto body = [&](auto blocks, int ad, int rows, int first, int count) __attribute__((always_inline)) {
-    constexpr int MB = decltype(blocks)::value;
-    int m[MB];
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb) {
-      const int j = first + mb * 16 + r16;
-      m[mb] = m0 + __shfl(rows, j < count ? j : 0, 64);
-    }
-    f32x4 acc[MB][4];
-#pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc[mb][e] = f32x4{0, 0, 0, 0};
-    const int rank = ad < 0 ? 0 : rank_of(a, ad);
+  // the rows whose bits are set in `mask`: of adapter ad (-1: none), or of none
+  auto body = [&](int ad, unsigned long long mask) __attribute__((always_inline)) {
+    const int list = nth_of(mask, lane), count = __builtin_popcountll(mask), first = wave * 16;
+    const bool busy = first < count;
     const uint16_t* up = a.b + max(ad, 0) * a.bs;
+    int m[4];                                       // rows of the results (behind the last: the first, not stored)
+    bool with[4];                                   // do they have the adapter?
 #pragma unroll
-    for (int rc = 0; rc < RC; ++rc) {
-      if (rc * 32 >= rank) break;
-      const int r = rc * 32 + 8 * q4;
-      const bool in = r < rank;
-      uint4 bf[4], tf[MB][PARTS];
+    for (int i = 0; i < 4; ++i) {
+      const int at = first + 4 * q4 + i, row = __shfl(list, at < count ? at : 0, 64);
+      m[i] = m0 + row;
+      with[i] = __shfl(mine, row, 64) >= 0;
+    }
+    // this lane's chunks of a block of B: read as far as R (what lies behind the rank is dropped below), the last row again behind N
+    uint4 bw[MINE];
+    auto load_b = [&](int nb) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int n = min(n0 + 16 * (r16 >> 2) + 4 * e + (r16 & 3), a.N - 1);           // behind the last: not stored
-        bf[e] = in ? load16(up + (int64_t)n * a.R + r) : zeros();
+      for (int i = 0; i < MINE; ++i) {
+        const int at = i * 64 * W + tid, row = at / CPR, ch = at % CPR;
+        bw[i] = load16(up + (int64_t)min(nb * 64 + row, a.N - 1) * a.R + min(8 * ch, a.R - 8));
       }
+    };
+    auto keep_b = [&](char* to, int rank) __attribute__((always_inline)) {
 #pragma unroll
-      for (int mb = 0; mb < MB; ++mb) {
-        float t[8] = {};
-        if (in) {
-          for (int z = 0; z < g.splits; ++z) {
-            const float* p = g.t + ((int64_t)z * a.M + m[mb]) * a.R + r;
-            const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+      for (int i = 0; i < MINE; ++i) {
+        const int at = i * 64 * W + tid, row = at / CPR, ch = at % CPR;
+        *reinterpret_cast<uint4*>(to + at_of(16 * (row & 3) + (row >> 2), ch)) = first_of(bw[i], rank - 8 * ch);
+      }
+    };
+    Run<F32> run[4];
+    auto load_base = [&](int nb) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) t[i] += lo[i], t[4 + i] += hi[i];
-          }
-        }
+      for (int i = 0; i < 4; ++i) run[i].load(a, g.vec, m[i], nb * 64 + 4 * r16);
+    };
+    // everything that is read goes under way before anything is waited for, the rank among it
+    if (ad >= 0) load_b(nb0);
+    if (busy) load_base(nb0);
+    const int row = __shfl(list, first + r16 < count ? first + r16 : 0, 64);
+    const bool has = __shfl(mine, row, 64) >= 0;
+    f32x4 tv[RC][2];
+    auto load_t = [&](int z, int rc, int i) __attribute__((always_inline)) {
+      return *reinterpret_cast<const f32x4*>(g.t + ((int64_t)z * a.M + m0 + row) * a.R + min(rc * 32 + 8 * q4, a.R - 8) + 4 * i);
+    };
+#pragma unroll
+    for (int rc = 0; rc < RC; ++rc)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) tv[rc][i] = ad >= 0 && busy ? load_t(0, rc, i) : f32x4{0, 0, 0, 0};
+    const int rank = ad < 0 ? 0 : rank_of(a, ad);
+    uint4 tf[RC][PARTS];
+    if (rank && busy) {
+      for (int z = 1; z < g.splits; ++z)
+#pragma unroll
+        for (int rc = 0; rc < RC; ++rc)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) tv[rc][i] += load_t(z, rc, i);
+#pragma unroll
+      for (int rc = 0; rc < RC; ++rc) {
+        const int held = has ? rank - rc * 32 - 8 * q4 : 0;                             // of this lane's eight ranks
+        float t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = i < held ? tv[rc][i / 4][i % 4] : 0.f;
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) {
           uint32_t w[4];
@@ -274,40 +353,57 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
             t[2 * i] = rest_of(t[2 * i], (uint16_t)w[i]);
             t[2 * i + 1] = rest_of(t[2 * i + 1], (uint16_t)(w[i] >> 16));
           }
-          tf[mb][p] = make_uint4(w[0], w[1], w[2], w[3]);
+          tf[rc][p] = make_uint4(w[0], w[1], w[2], w[3]);
         }
       }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const bf16x8 b = as_bf16x8(first_of(bf[e], rank - r));
-#pragma unroll
-        for (int mb = 0; mb < MB; ++mb)
-#pragma unroll
-          for (int p = 0; p < PARTS; ++p) acc[mb][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, as_bf16x8(tf[mb][p]), acc[mb][e], 0, 0, 0);
-      }
     }
-    // lane holds outputs n0 + 16 q4 + 4 e + i of its rows
+    __syncthreads();                                // (the last adapter's block has been read)
+    if (rank) keep_b(lds[0], rank);
+    __syncthreads();
+    for (int nb = nb0; nb < nb1; ++nb) {
+      const char* b = lds[(nb - nb0) & 1];
+      if (rank && nb + 1 < nb1) load_b(nb + 1);
+      if (busy) {
+        f32x4 acc[4];
 #pragma unroll
-    for (int mb = 0; mb < MB; ++mb)
-      if (first + mb * 16 + r16 < count) finish<F32>(a, g.vec, m[mb], n0 + 16 * q4, acc[mb]);
-  };
-  auto rows_of = [&](unsigned long long mask, int ad) __attribute__((always_inline)) {
-    const int rows = nth_of(mask, lane), count = __builtin_popcountll(mask);
-    if (count > 32) {
-      body(std::integral_constant<int, 4>(), ad, rows, 0, count);
-    } else {
-      for (int first = 0; first < count; first += 16) body(std::integral_constant<int, 1>(), ad, rows, first, count);
+        for (int e = 0; e < 4; ++e) acc[e] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int rc = 0; rc < RC; ++rc)
+          if (rc * 32 < rank) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bf16x8 bf = as_bf16x8(load16(b + at_of(16 * e + r16, 4 * rc + q4)));
+#pragma unroll
+              for (int p = 0; p < PARTS; ++p) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(tf[rc][p]), bf, acc[e], 0, 0, 0);
+            }
+          }
+        Run<F32> now[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) now[i] = run[i];
+        if (nb + 1 < nb1) load_base(nb + 1);
+        // lane holds outputs 64 nb + 4 r16 + e of rows 4 q4 + i
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (first + 4 * q4 + i < count)
+            now[i].finish(a, g.vec, m[i], nb * 64 + 4 * r16, with[i] ? f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]} : f32x4{0, 0, 0, 0});
+      }
+      if (rank && nb + 1 < nb1) {
+        keep_b(lds[(nb + 1 - nb0) & 1], rank);
+        __syncthreads();
+      }
     }
   };
   unsigned long long left = __ballot(mine >= 0);
+  // rows without an adapter go with the first adapter's, or by themselves
   const unsigned long long none = __ballot(m0 + lane < a.M) & ~left;
-  if (slot == 0 && none) rows_of(none, -1);
-  for (int j = 0; left; ++j) {
-    const int ad = __builtin_amdgcn_readlane(mine, (int)__builtin_ctzll(left));
-    const unsigned long long mask = __ballot(mine == ad);
+  int j = 0;
+  do {
+    const int ad = left ? __builtin_amdgcn_readlane(mine, (int)__builtin_ctzll(left)) : -1;
+    const unsigned long long mask = __ballot(mine == ad) & left;
     left &= ~mask;
-    if (j % g.slots == slot) rows_of(mask, ad);
-  }
+    if (j % g.slots == slot) body(ad, j ? mask : mask | none);
+    ++j;
+  } while (left);
 }
 
 // Both products in one launch, for 16 rows and 256 outputs; every adapter's results are chosen for its rows.
@@ -333,8 +429,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
   uint32_t left = (uint32_t)__ballot(mine >= 0) & 0xffffu;
   while (left) {
     const int ad = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
-    const bool on = mine == ad;
-    left &= ~(uint32_t)__ballot(on);
+    left &= ~(uint32_t)__ballot(mine == ad);
     const int rank = rank_of(a, ad);
     if (rank == 0) continue;
     const uint16_t* down = a.a + ad * a.as;
@@ -388,23 +483,35 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
       for (int p = 0; p < PARTS; ++p) tf[p] = as_bf16x8(load16(&ts[p][r16][r]));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int n = n0 + 16 * (r16 >> 2) + 4 * e + (r16 & 3);
+        const int n = n0 + 4 * r16 + e;
         const uint4 bf = n < a.N && r < rank ? first_of(load16(up + (int64_t)n * a.R + r), rank - r) : zeros();
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) y[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(bf), tf[p], y[e], 0, 0, 0);
+        for (int p = 0; p < PARTS; ++p) y[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tf[p], as_bf16x8(bf), y[e], 0, 0, 0);
       }
     }
-    if (on) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) acc[e] = y[e];
+    for (int i = 0; i < 4; ++i) {
+      if (__shfl(mine, 4 * q4 + i, 64) != ad) continue;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e][i] = y[e][i];
     }
   }
-  // lane holds outputs n0 + 16 q4 + 4 e + i of its row
-  if (row) finish<F32>(a, g.vec, m, n0 + 16 * q4, acc);
+  // lane holds outputs n0 + 4 r16 + e of rows 4 q4 + i
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int to = m0 + 4 * q4 + i;
+    if (to >= a.M) continue;
+    Run<F32> run;
+    run.load(a, g.vec, to, n0 + 4 * r16);
+    run.finish(a, g.vec, to, n0 + 4 * r16, f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]});
+  }
 }
 
 template <bool F32>
-hipError_t up(const LoraArgs& g, unsigned wgs, hipStream_t s) {
+hipError_t up(LoraArgs g, hipStream_t s) {
+  const int tiles = (g.a.M + 63) / 64;
+  g.xcds = tiles < 8 ? 1 : 8;
+  const unsigned wgs = (unsigned)((tiles + g.xcds - 1) / g.xcds * g.xcds) * g.slots * g.tiles_n;
   const int rc = (g.a.R + 31) / 32;
   return launch(rc == 1 ? k_lora_up<F32, 1> : rc == 2 ? k_lora_up<F32, 2> : k_lora_up<F32, 4>, dim3(wgs), dim3(256), 0, s, g);
 }
@@ -419,8 +526,8 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   g.a = a;
   g.t = sp.partials;
   g.tiles_n = (int)(((int64_t)a.N + 255) / 256);
-  const int64_t run = a.f32 ? 4 : 8;
-  g.vec = (uintptr_t)a.y % 16 == 0 && a.ldy % run == 0 && (uintptr_t)a.base % 16 == 0 && (!a.base || a.ldbase % run == 0);
+  const uintptr_t four = a.f32 ? 16 : 8;
+  g.vec = (uintptr_t)a.y % four == 0 && a.ldy % 4 == 0 && (uintptr_t)a.base % four == 0 && a.ldbase % 4 == 0;
   if (((int64_t)a.M + 15) / 16 * g.tiles_n >= 1 << 24) return hipErrorInvalidValue;
   const LoraPlan p = lora_plan(a.M, a.N, a.K, a.R, a.adapters, sp.partials ? sp.partial_bytes : 0);
   if (p.splits == 0)
@@ -429,12 +536,16 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   g.slots = p.down_slots;
   const unsigned tiles = (a.M + 31) / 32;
   const int rb = (a.R + 15) / 16;
-  const hipError_t e = launch(rb == 1 ? k_lora_down<1, 8> : rb == 2 ? k_lora_down<2, 8> : rb <= 4 ? k_lora_down<4, 8> : k_lora_down<8, 8>,
-                              dim3(tiles * g.slots * g.splits), dim3(512), 0, s, g);
+  const unsigned down = tiles * g.slots * g.splits;
+  const hipError_t e = rb == 1   ? launch(k_lora_down<1, 4, 2>, dim3(down), dim3(256), 0, s, g)
+                       : rb == 2 ? launch(k_lora_down<2, 4, 2>, dim3(down), dim3(256), 0, s, g)
+                       : rb <= 4 ? launch(k_lora_down<4, 3, 2>, dim3(down), dim3(192), 0, s, g)
+                                 : launch(k_lora_down<8, 4, 1>, dim3(down), dim3(256), 0, s, g);
   if (e != hipSuccess) return e;
   g.slots = p.up_slots;
-  const unsigned wgs = (unsigned)((a.M + 63) / 64) * g.slots * g.tiles_n;
-  return a.f32 ? up<true>(g, wgs, s) : up<false>(g, wgs, s);
+  g.run = p.run;
+  g.tiles_n = (int)((((int64_t)a.N + 63) / 64 + g.run - 1) / g.run);
+  return a.f32 ? up<true>(g, s) : up<false>(g, s);
 }
 
 }  // namespace k
