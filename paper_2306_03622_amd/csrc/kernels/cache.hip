@@ -1,147 +1,172 @@
 // Rows of keys and values into the pages of a cache and out of them (torpor_serve.h), on gfx950.
 //
-// A lane moves eight values, D / 8 lanes one token's head; rows are numbered sequence, row, k or v, head, so that
-// lanes side by side read and write what lies side by side in the usual layouts. Each lane finds its page by itself: two lengths
-// and a table entry, which the lanes of a token share in the caches.
+// A lane moves eight values of a key and of its value, D / 8 lanes one token's head, lanes side by side what lies side by side in the
+// usual layouts. A workgroup belongs to one sequence and takes U rows in each place, all of whose pages and then values are asked for
+// before the first is waited for. What is left of the index arithmetic is scalar or once a lane (by divisions in every lane, reading 8191
+// tokens of 8 heads of 128 in 8 bits took 14.8 us, now 10.5).
 //
-// 8-bit rows: a = max |x| over the finite values of the head (a butterfly over its lanes), s = 2^e the smallest power of two
+// 8-bit rows: a = max |x| over the finite values of the head, s = 2^e the smallest power of two
 // with a <= 448 s = 1.75 2^8 s: for a = m 2^x, 1 <= m < 2, e = x - 8, or x - 7 where m > 1.75. Division by s is exact (a power of two), so
 // the one rounding is the conversion's. Reading back, code * s has four significant bits: exact in bf16 unless it leaves its range.
 #include "serve_args.hpp"
 
 namespace tp {
 namespace k {
-namespace {
 
-// Where lane `id` of a call works: sequence, row, k or v, head, chunk of eight values, page (negative: none) and token of it.
-struct Place {
-  int b, i, kv, h, ch, page, at;
-  bool row;                         // a row that the sequence has
+struct CacheRowsArgs {
+  CacheRows a;
+  int per, cols;          // lanes that a token takes, workgroups side by side for one (more than 1: then a row at a time)
+  int rows, blocks;       // rows side by side in a workgroup, workgroups along the rows
 };
 
+template <>
+struct PtrFields<CacheRowsArgs> {
+  static void add(std::vector<uint32_t>& v, uint32_t at) { PtrFields<CacheRows>::add(v, at + (uint32_t)offsetof(CacheRowsArgs, a)); }
+};
+
+namespace {
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, false));
+}
+
+// Eight values of a head in 8 bits: the head's exponent byte, the codes.
 template <int CPH>
-__device__ __forceinline__ Place place_of(const CacheRows& a, int id) {
-  Place p;
-  p.ch = id % CPH;
-  int v = id / CPH;
-  p.h = v % a.c.heads;
-  v /= a.c.heads;
-  p.kv = v & 1;
-  v >>= 1;
-  p.i = v % a.p.q_len;
-  p.b = v / a.p.q_len;
-  const Lens l = lens_of(a.p, p.b);
-  p.row = p.i < l.qn;
-  const int pos = l.kn - l.qn + p.i, col = pos >> a.c.lg;
-  p.page = -1;
-  if (p.row && pos >= 0 && col < a.p.max_pages) {
-    const int page = a.p.table[(int64_t)p.b * a.p.table_stride + col];
-    if ((unsigned)page < (unsigned)a.c.pages) p.page = page;
+__device__ __forceinline__ uint2 to_e4m3(uint4 w, int* byte) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+  uint32_t top = 0;                                 // bf16 bits of the largest finite magnitude
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const uint32_t lo = u[j] & 0x7fffu, hi = u[j] >> 16 & 0x7fffu;
+    top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
   }
-  p.at = pos & ((1 << a.c.lg) - 1);
-  return p;
+  // over the head's lanes, all of which are there: mirrored in 16 and in 8 lanes, then inside four
+  if constexpr (CPH == 16) top = dpp_max<0x140>(top);
+  top = dpp_max<0x141>(top);
+  top = dpp_max<0x4E>(top);
+  top = dpp_max<0xB1>(top);
+  // exponent bits of a, and one more where its seven mantissa bits are over those of 1.75
+  *byte = max((int)((top + 0x1fu) >> 7) - 8, 1);
+  const float inv = __uint_as_float((uint32_t)(254 - *byte) << 23);
+  uint32_t c[2];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(u[2 * j] << 16) * inv, __uint_as_float(u[2 * j] & 0xffff0000u) * inv, 0, false);
+    c[j] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(__uint_as_float(u[2 * j + 1] << 16) * inv, __uint_as_float(u[2 * j + 1] & 0xffff0000u) * inv, lo, true);
+  }
+  return make_uint2(c[0], c[1]);
 }
 
-__device__ __forceinline__ uint16_t* row_at(const CacheRows& a, const Place& p) {
-  const int64_t* s = p.kv ? a.rvs : a.rks;
-  return (p.kv ? a.v : a.k) + p.b * s[0] + p.i * s[1] + p.h * s[2] + 8 * p.ch;
-}
-template <bool E4M3>
-__device__ __forceinline__ char* cell_at(const CacheRows& a, const Place& p) {
-  const int64_t* s = p.kv ? a.c.vs : a.c.ks;
-  return static_cast<char*>(p.kv ? a.c.v : a.c.k) + p.page * s[0] + p.at * s[1] + p.h * s[2] + (E4M3 ? 8 : 16) * p.ch;
-}
-__device__ __forceinline__ uint8_t* exp_at(const CacheRows& a, const Place& p) {
-  return a.c.exps + ((((int64_t)p.page * 2 + p.kv) * a.c.heads + p.h) << a.c.lg) + p.at;
+__device__ __forceinline__ uint4 from_e4m3(uint2 c, uint32_t byte) {
+  const float s = __uint_as_float(byte << 23);
+  auto two = [&](uint32_t x, auto high) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, decltype(high)::value));
+    return f2bf2(__uint_as_float(b << 16) * s, __uint_as_float(b & 0xffff0000u) * s);
+  };
+  return make_uint4(two(c.x, std::false_type()), two(c.x, std::true_type()), two(c.y, std::false_type()), two(c.y, std::true_type()));
 }
 
-template <int D, bool E4M3>
-__global__ __launch_bounds__(256) void k_cache_append(CacheRows a, int lanes) {
-  constexpr int CPH = D / 8;
-  const int id = blockIdx.x * 256 + threadIdx.x;
-  const Place p = place_of<CPH>(a, min(id, lanes - 1));
-  const bool live = id < lanes && p.page >= 0;      // the same for the lanes of a head
-  if (!live) return;
-  const uint4 w = *reinterpret_cast<const uint4*>(row_at(a, p));
-  char* cell = cell_at<E4M3>(a, p);
-  if constexpr (!E4M3) {
-    *reinterpret_cast<uint4*>(cell) = w;
+template <int D, bool E4M3, bool APPEND, int U>
+__global__ __launch_bounds__(256) void k_cache_rows(CacheRowsArgs g) {
+  constexpr int CPH = D / 8, CELL = E4M3 ? 8 : 16;
+  const CacheRows& a = g.a;
+  const Cache& c = a.c;
+  int id = blockIdx.x;
+  const int col = id % g.cols;
+  id /= g.cols;
+  const int block = id % g.blocks, b = id / g.blocks;
+  const int sub = g.rows > 1 ? (int)threadIdx.x / g.per : 0, lane = (int)threadIdx.x - sub * g.per + col * 256;
+  if (sub >= g.rows || lane >= g.per) return;       // whole heads
+  const int h = lane / CPH, ch = lane % CPH;
+  const Lens l = lens_of(a.p, b);
+  const int32_t* table = a.p.table + b * a.p.table_stride;
+  uint16_t* const rows[2] = {a.k + b * a.rks[0] + h * a.rks[2] + 8 * ch, a.v + b * a.rvs[0] + h * a.rvs[2] + 8 * ch};
+  char* const cells[2] = {static_cast<char*>(c.k) + h * c.ks[2] + CELL * ch, static_cast<char*>(c.v) + h * c.vs[2] + CELL * ch};
+
+  int row[U], page[U], at[U];
+  auto row_at = [&](int n, int u) { return reinterpret_cast<uint4*>(rows[n] + row[u] * (n ? a.rvs[1] : a.rks[1])); };
+  uint4 w[2][U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    row[u] = (block * U + u) * g.rows + sub;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) w[n][u] = APPEND && row[u] < l.qn ? *row_at(n, u) : make_uint4(0, 0, 0, 0);
+    const int pos = l.kn - l.qn + row[u], k = pos >> c.lg;
+    page[u] = -1;
+    at[u] = pos & ((1 << c.lg) - 1);
+    if (row[u] < l.qn && pos >= 0 && k < a.p.max_pages) page[u] = table[k];
+    if ((unsigned)page[u] >= (unsigned)c.pages) page[u] = -1;
+  }
+  auto cell_at = [&](int n, int u) { return cells[n] + page[u] * (n ? c.vs[0] : c.ks[0]) + at[u] * (n ? c.vs[1] : c.ks[1]); };
+  auto exp_at = [&](int n, int u) { return c.exps + ((((int64_t)page[u] * 2 + n) * c.heads + h) << c.lg) + at[u]; };
+  if constexpr (APPEND) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int n = 0; n < 2; ++n) {
+        if (page[u] < 0) continue;                  // the same for the lanes of a head
+        if constexpr (E4M3) {
+          int byte;
+          *reinterpret_cast<uint2*>(cell_at(n, u)) = to_e4m3<CPH>(w[n][u], &byte);
+          if (ch == 0) *exp_at(n, u) = (uint8_t)byte;
+        } else {
+          *reinterpret_cast<uint4*>(cell_at(n, u)) = w[n][u];
+        }
+      }
   } else {
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-    uint32_t top = 0;                               // bf16 bits of the largest finite magnitude
+    uint32_t byte[2][U];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t lo = u[j] & 0x7fffu, hi = u[j] >> 16 & 0x7fffu;
-      top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-    }
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int m = CPH / 2; m > 0; m >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, m, 64));
-    // exponent bits of a, and one more where its seven mantissa bits are over those of 1.75
-    const int byte = max((int)((top + 0x1fu) >> 7) - 8, 1);
-    const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);
-    uint32_t c[2] = {0, 0};
+      for (int n = 0; n < 2; ++n) {
+        byte[n][u] = 0;
+        if (page[u] < 0) continue;
+        if constexpr (E4M3) {
+          const uint2 x = *reinterpret_cast<const uint2*>(cell_at(n, u));
+          w[n][u].x = x.x, w[n][u].y = x.y;
+          byte[n][u] = *exp_at(n, u);
+        } else {
+          w[n][u] = *reinterpret_cast<const uint4*>(cell_at(n, u));
+        }
+      }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float lo = __uint_as_float(u[j] << 16) * inv, hi = __uint_as_float(u[j] & 0xffff0000u) * inv;
-      const uint32_t pair = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(lo, hi, 0, false) & 0xffffu;
-      c[j / 2] |= pair << (16 * (j & 1));
-    }
-    *reinterpret_cast<uint2*>(cell) = make_uint2(c[0], c[1]);
-    if (p.ch == 0) *exp_at(a, p) = (uint8_t)byte;
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+        if (row[u] < l.qn) *row_at(n, u) = E4M3 && page[u] >= 0 ? from_e4m3(make_uint2(w[n][u].x, w[n][u].y), byte[n][u]) : w[n][u];
   }
 }
 
-template <int D, bool E4M3>
-__global__ __launch_bounds__(256) void k_cache_read(CacheRows a, int lanes) {
-  constexpr int CPH = D / 8;
-  const int id = blockIdx.x * 256 + threadIdx.x;
-  if (id >= lanes) return;
-  const Place p = place_of<CPH>(a, id);
-  if (!p.row) return;
-  uint4 w = make_uint4(0, 0, 0, 0);
-  if (p.page >= 0) {
-    const char* cell = cell_at<E4M3>(a, p);
-    if constexpr (!E4M3) {
-      w = *reinterpret_cast<const uint4*>(cell);
-    } else {
-      const uint2 c = *reinterpret_cast<const uint2*>(cell);
-      const float s = __uint_as_float((uint32_t)*exp_at(a, p) << 23);
-      auto two = [&](uint32_t x, auto high) {
-        const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, decltype(high)::value);
-        const uint32_t b = __builtin_bit_cast(uint32_t, v);
-        return f2bf2(__uint_as_float(b << 16) * s, __uint_as_float(b & 0xffff0000u) * s);
-      };
-      w = make_uint4(two(c.x, std::false_type()), two(c.x, std::true_type()), two(c.y, std::false_type()), two(c.y, std::true_type()));
-    }
-  }
-  *reinterpret_cast<uint4*>(row_at(a, p)) = w;
+template <int D, bool E4M3, bool APPEND>
+hipError_t go(CacheRowsArgs g, int64_t wgs, int u, hipStream_t s) {
+  return launch(u == 1 ? k_cache_rows<D, E4M3, APPEND, 1> : k_cache_rows<D, E4M3, APPEND, 2>, dim3((unsigned)wgs), dim3(256), 0, s, g);
 }
 
-// Lanes of a call, or 0 for one that the kernels cannot take.
-int lanes_of(const CacheRows& a) {
+template <bool APPEND>
+hipError_t rows(const CacheRows& a, hipStream_t s) {
   if (!a.c.k || !a.c.v || (a.c.e4m3 && !a.c.exps) || !a.p.table || !a.p.kv_lens || !a.k || !a.v || (a.c.dim != 64 && a.c.dim != 128) ||
-      a.p.batch < 1 || a.p.q_len < 1 || a.c.heads < 1 || a.c.pages < 1 || a.p.max_pages < 1 || a.c.lg < 4 || a.c.lg > 12)
-    return 0;
-  const int64_t heads = (int64_t)a.p.batch * a.p.q_len * a.c.heads;
-  return heads < 1 << 26 ? (int)(heads * 2 * (a.c.dim / 8)) : 0;
-}
-
-template <typename F64, typename F128>
-hipError_t go(const CacheRows& a, hipStream_t s, F64 k64, F128 k128) {
-  const int lanes = lanes_of(a);
-  if (!lanes) return hipErrorInvalidValue;
-  return launch(a.c.dim == 64 ? k64 : k128, dim3(((unsigned)lanes + 255) / 256), dim3(256), 0, s, a, lanes);
+      a.p.batch < 1 || a.p.q_len < 1 || a.c.heads < 1 || a.c.heads > 65536 || a.c.pages < 1 || a.p.max_pages < 1 || a.c.lg < 4 || a.c.lg > 12)
+    return hipErrorInvalidValue;
+  CacheRowsArgs g{};
+  g.a = a;
+  g.per = a.c.heads * (a.c.dim / 8);
+  g.cols = (g.per + 255) / 256;
+  g.rows = g.cols > 1 ? 1 : 256 / g.per;
+  // two rows in each place where that still gives every CU two workgroups (two prompts of 3001 in 8 bits 8.8 us, with four 9.8, one 9.4)
+  auto blocks = [&](int u) { return ((int64_t)a.p.q_len + (int64_t)g.rows * u - 1) / ((int64_t)g.rows * u); };
+  const int u = blocks(2) * g.cols * a.p.batch >= 512 ? 2 : 1;
+  const int64_t wgs = blocks(u) * g.cols * a.p.batch;
+  if (wgs >= 1 << 24) return hipErrorInvalidValue;
+  g.blocks = (int)blocks(u);
+  if (a.c.e4m3) return a.c.dim == 64 ? go<64, true, APPEND>(g, wgs, u, s) : go<128, true, APPEND>(g, wgs, u, s);
+  return a.c.dim == 64 ? go<64, false, APPEND>(g, wgs, u, s) : go<128, false, APPEND>(g, wgs, u, s);
 }
 
 }  // namespace
 
-hipError_t cache_append(const CacheRows& a, hipStream_t s) {
-  return a.c.e4m3 ? go(a, s, k_cache_append<64, true>, k_cache_append<128, true>) : go(a, s, k_cache_append<64, false>, k_cache_append<128, false>);
-}
-
-hipError_t cache_read(const CacheRows& a, hipStream_t s) {
-  return a.c.e4m3 ? go(a, s, k_cache_read<64, true>, k_cache_read<128, true>) : go(a, s, k_cache_read<64, false>, k_cache_read<128, false>);
-}
+hipError_t cache_append(const CacheRows& a, hipStream_t s) { return rows<true>(a, s); }
+hipError_t cache_read(const CacheRows& a, hipStream_t s) { return rows<false>(a, s); }
 
 }  // namespace k
 }  // namespace tp

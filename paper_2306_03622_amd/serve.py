@@ -59,23 +59,18 @@ def _serve_calls():
     return _calls
 
 
-def _made(torch, current, here, call, packed, dev, stream):
-    """Makes the call on `stream` (None: the device's current one) with the tensors' device the current one where that matters."""
-    s = current(dev) if stream is None else _stream_of(dev, stream)
-    if s or here() == dev:                # the null stream is that of whichever device is current; any other carries its own
-        status = call(packed, s)
-    else:
-        with torch.cuda.device(dev):
-            status = call(packed, s)
-    if status != TP_OK:
-        _check(lib(), status)
+def _on_device(torch, call, packed, dev, stream):
+    """The call's status, made with the tensors' device the current one."""
+    with torch.cuda.device(dev):
+        return call(packed, stream)
 
+
+# What the calls check they check in place, all at once, since a function call for each tensor took 1 us of a 6.5 us call; the functions
+# below then say what is wrong.
 
 def _ints(name, t, n, torch, dev):
-    """Address of a contiguous int32 [n] on the device."""
-    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous() or t.get_device() != dev:
+    if t.dtype is not torch.int32 or t.numel() != n or not t.is_contiguous() or t.get_device() != dev:
         raise ValueError(f"{name} must be a contiguous int32 [{n}] on device {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
 
 
 def _scratch(t, dev):
@@ -83,6 +78,28 @@ def _scratch(t, dev):
     if t.get_device() != dev or not t.is_contiguous():
         raise ValueError(f"work must be contiguous and on device {dev}, not {tuple(t.shape)} by {t.stride()} on {t.device}")
     return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _heads(name, t, bf, dev):
+    if t.dtype is not bf:
+        raise ValueError(f"{name} is {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the cache on device {dev}")
+    if t.stride(3) != 1:
+        raise ValueError(f"{name}: the values of a head must be contiguous")
+
+
+def _wrong(torch, dev, batch, table, kv_lens, q_lens, **heads):
+    """Raises for the first of the tensors that a call on a cache cannot take."""
+    for name, t in heads.items():
+        _heads(name, t, torch.bfloat16, dev)
+    if table.dtype is not torch.int32 or table.dim() != 2 or table.shape[0] != batch or table.get_device() != dev:
+        raise ValueError(f"table must be int32 [{batch}][pages] on device {dev}, not {table.dtype} {tuple(table.shape)} on {table.device}")
+    if table.shape[1] > 1 and table.stride(1) != 1:
+        raise ValueError("table: rows must be contiguous")
+    _ints("kv_lens", kv_lens, batch, torch, dev)
+    if q_lens is not None:
+        _ints("q_lens", q_lens, batch, torch, dev)
 
 
 class PagedCache:
@@ -113,7 +130,7 @@ class PagedCache:
                              TPS_E4M3 if e4m3 else TP_BF16, pages, size, heads, dim, 0)
         # tensor objects of its own hold the memory: the caller's may be given other memory (t.data = ..)
         for name, value in (("_k", k.detach()), ("_v", v.detach()), ("_exps", exps.detach() if e4m3 else None), ("device", k.device),
-                            ("_packed", (k.device.index, packed)), ("pages", pages), ("page_size", size), ("kv_heads", heads),
+                            ("_packed", (k.device.index, packed, heads, dim, size)), ("pages", pages), ("page_size", size), ("kv_heads", heads),
                             ("head_dim", dim), ("e4m3", e4m3)):
             object.__setattr__(self, name, value)
 
@@ -135,41 +152,30 @@ class PagedCache:
         return cls(k, v, torch.empty(pages, 2, kv_heads, page_size, dtype=torch.uint8, device=device) if e4m3 else None)
 
 
-def _table(table, batch, torch, dev):
-    """(address, row stride, columns) of a table of pages."""
-    if table.dtype is not torch.int32 or table.dim() != 2 or table.shape[0] != batch or table.get_device() != dev:
-        raise ValueError(f"table must be int32 [{batch}][pages] on device {dev}, not {table.dtype} {tuple(table.shape)} on {table.device}")
-    if table.shape[1] > 1 and table.stride(1) != 1:
-        raise ValueError("table: rows must be contiguous")
-    return table.data_ptr(), table.stride(0), table.shape[1]
-
-
-def _heads(name, t, bf, dev):
-    """Raises for a tensor of heads that a call cannot take."""
-    if t.dtype is not bf:
-        raise ValueError(f"{name} is {t.dtype}")
-    if t.get_device() != dev:
-        raise ValueError(f"{name} is on {t.device}, the cache on device {dev}")
-    if t.stride(3) != 1:
-        raise ValueError(f"{name}: the values of a head must be contiguous")
-
-
 def _rows(which, cache, table, kv_lens, k, v, q_lens, stream):
     calls = _calls or _serve_calls()
     torch, current, here = calls[:3]
-    dev, packed = cache._packed
-    if k.dim() != 4 or v.shape != k.shape or k.shape[2] != cache.kv_heads or k.shape[3] != cache.head_dim:
-        raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}, a cache of {cache.kv_heads} heads of {cache.head_dim}")
-    b, n = k.shape[:2]
-    for name, t in (("k", k), ("v", v)):
-        _heads(name, t, torch.bfloat16, dev)
-    tp, ts, columns = _table(table, b, torch, dev)
-    kl = _ints("kv_lens", kv_lens, b, torch, dev)
-    ql = 0 if q_lens is None else _ints("q_lens", q_lens, b, torch, dev)
-    k0, k1, k2, _ = k.stride()
-    v0, v1, v2, _ = v.stride()
-    packed += _ROWS.pack(tp, ts, ql, kl, k.data_ptr(), v.data_ptr(), k0, k1, k2, v0, v1, v2, b, n, columns, 0)
-    _made(torch, current, here, calls[which], packed, dev, stream)
+    dev, packed, heads, dim, _ = cache._packed
+    shape = k.shape
+    if len(shape) != 4 or v.shape != shape or shape[2] != heads or shape[3] != dim:
+        raise ValueError(f"k {tuple(k.shape)}, v {tuple(v.shape)}, a cache of {heads} heads of {dim}")
+    b, n = shape[0], shape[1]
+    bf, i32 = torch.bfloat16, torch.int32
+    k0, k1, k2, k3 = k.stride()
+    v0, v1, v2, v3 = v.stride()
+    if not (k.dtype is v.dtype is bf and table.dtype is kv_lens.dtype is i32 and k3 == v3 == 1 and table.dim() == 2 and
+            k.get_device() == v.get_device() == table.get_device() == kv_lens.get_device() == dev and kv_lens.numel() == b and
+            kv_lens.is_contiguous() and table.shape[0] == b and table.stride(1) == 1 and
+            (q_lens is None or (q_lens.dtype is i32 and q_lens.numel() == b and q_lens.is_contiguous() and q_lens.get_device() == dev))):
+        _wrong(torch, dev, b, table, kv_lens, q_lens, k=k, v=v)
+    columns = table.shape[1]
+    packed += _ROWS.pack(table.data_ptr(), table.stride(0), 0 if q_lens is None else q_lens.data_ptr(), kv_lens.data_ptr(), k.data_ptr(),
+                         v.data_ptr(), k0, k1, k2, v0, v1, v2, b, n, columns, 0)
+    s = current(dev) if stream is None else _stream_of(dev, stream)
+    # the null stream is that of whichever device is current; any other carries its own
+    status = calls[which](packed, s) if s or here() == dev else _on_device(torch, calls[which], packed, dev, s)
+    if status != TP_OK:
+        _check(lib(), status)
 
 
 def tps_cache_append(cache: PagedCache, table, kv_lens, k, v, q_lens=None, stream=None):
@@ -189,25 +195,29 @@ def tps_cache_attention(cache: PagedCache, table, kv_lens, q, out, q_lens=None, 
     """Attention of the new tokens' q [B][q_len][heads][dim] over the cache, which holds their keys and values already, into out
     (as q), bf16, in causal order. kv_len: no sequence is longer (default: what the table has room for); window: keys to the
     left of a token that it sees (negative: all); sinks: first keys that it sees besides; see torpor_serve.h."""
-    calls = _calls or _serve_calls()
-    torch, current, here = calls[:3]
-    dev, packed = cache._packed
-    if q.dim() != 4 or out.shape != q.shape or q.shape[3] != cache.head_dim:
-        raise ValueError(f"q {tuple(q.shape)}, out {tuple(out.shape)}, a cache of heads of {cache.head_dim}")
-    b, n, h, _ = q.shape
+    torch, current, here, _, _, call, _ = _calls or _serve_calls()
+    dev, packed, _, dim, size = cache._packed
+    shape = q.shape
+    if len(shape) != 4 or out.shape != shape or shape[3] != dim:
+        raise ValueError(f"q {tuple(q.shape)}, out {tuple(out.shape)}, a cache of heads of {dim}")
+    b, n, h, _ = shape
     q0, q1, q2, q3 = q.stride()
     o0, o1, o2, o3 = out.stride()
-    bf = torch.bfloat16
-    if not (q.dtype is out.dtype is bf and q3 == o3 == 1 and q.get_device() == out.get_device() == dev):
-        for name, t in (("q", q), ("out", out)):
-            _heads(name, t, bf, dev)
-    tp, ts, columns = _table(table, b, torch, dev)
-    kl = _ints("kv_lens", kv_lens, b, torch, dev)
-    ql = 0 if q_lens is None else _ints("q_lens", q_lens, b, torch, dev)
+    i32 = torch.int32
+    if not (q.dtype is out.dtype is torch.bfloat16 and table.dtype is kv_lens.dtype is i32 and q3 == o3 == 1 and table.dim() == 2 and
+            q.get_device() == out.get_device() == table.get_device() == kv_lens.get_device() == dev and kv_lens.numel() == b and
+            kv_lens.is_contiguous() and table.shape[0] == b and table.stride(1) == 1 and
+            (q_lens is None or (q_lens.dtype is i32 and q_lens.numel() == b and q_lens.is_contiguous() and q_lens.get_device() == dev))):
+        _wrong(torch, dev, b, table, kv_lens, q_lens, q=q, out=out)
+    columns = table.shape[1]
     wp, wb = (0, 0) if work is None else _scratch(work, dev)
-    packed += _ATTENTION.pack(tp, ts, ql, kl, q.data_ptr(), out.data_ptr(), q0, q1, q2, o0, o1, o2, b, h, n,
-                              columns * cache.page_size if kv_len is None else kv_len, columns, window, sinks, scale, wp, wb)
-    _made(torch, current, here, calls[5], packed, dev, stream)
+    packed += _ATTENTION.pack(table.data_ptr(), table.stride(0), 0 if q_lens is None else q_lens.data_ptr(), kv_lens.data_ptr(), q.data_ptr(),
+                              out.data_ptr(), q0, q1, q2, o0, o1, o2, b, h, n, columns * size if kv_len is None else kv_len, columns, window,
+                              sinks, scale, wp, wb)
+    s = current(dev) if stream is None else _stream_of(dev, stream)
+    status = call(packed, s) if s or here() == dev else _on_device(torch, call, packed, dev, s)
+    if status != TP_OK:
+        _check(lib(), status)
 
 
 def tps_lora(x, a, b, adapter, out, base=None, ranks=None, scales=None, act: str = "none", work=None, stream=None):
@@ -218,38 +228,45 @@ def tps_lora(x, a, b, adapter, out, base=None, ranks=None, scales=None, act: str
     bf, dev = torch.bfloat16, x.get_device()
     if dev < 0:
         raise ValueError(f"x on {x.device}")
-    if x.dim() != 2 or a.dim() != 3 or b.dim() != 3 or out.dim() != 2:
+    xs, ash, os = x.shape, a.shape, out.shape
+    if len(xs) != 2 or len(ash) != 3 or len(os) != 2 or ash[2] != xs[1] or os[0] != xs[0] or b.shape != (ash[0], os[1], ash[1]):
         raise ValueError(f"x {tuple(x.shape)}, a {tuple(a.shape)}, b {tuple(b.shape)}, out {tuple(out.shape)}")
-    m, k = x.shape
-    slots, r, ka = a.shape
-    n = out.shape[1]
-    if ka != k or b.shape != (slots, n, r) or out.shape[0] != m:
-        raise ValueError(f"x {tuple(x.shape)}, a {tuple(a.shape)}, b {tuple(b.shape)}, out {tuple(out.shape)}")
+    m, k = xs
+    slots, r, _ = ash
+    n = os[1]
     f32 = out.dtype is torch.float32
     a0, a1, a2 = a.stride()
     b0, b1, b2 = b.stride()
+    x0, x1 = x.stride()
+    o0, o1 = out.stride()
     if not (x.dtype is a.dtype is b.dtype is bf and (f32 or out.dtype is bf)):
         raise ValueError(f"x {x.dtype}, a {a.dtype}, b {b.dtype}, out {out.dtype}")
     if not (a.get_device() == b.get_device() == out.get_device() == dev):
         raise ValueError(f"x on device {dev}, a on {a.device}, b on {b.device}, out on {out.device}")
-    if (k > 1 and x.stride(1) != 1) or (n > 1 and out.stride(1) != 1):
+    if x1 != 1 or (o1 != 1 and n > 1):
         raise ValueError("rows of x and out must be contiguous")
-    if a2 != 1 or b2 != 1 or a1 != k or (n > 1 and b1 != r):
+    if a2 != 1 or b2 != 1 or a1 != k or (b1 != r and n > 1):
         raise ValueError("every adapter's matrices must be contiguous")
     bp = ldb = rp = sp = wp = wb = 0
     if base is not None:
-        if base.dtype is not out.dtype or base.shape != out.shape or base.get_device() != dev or (n > 1 and base.stride(1) != 1):
+        ldb, base1 = base.stride() if base.dim() == 2 else (0, 0)
+        if base.dtype is not out.dtype or base.shape != os or base.get_device() != dev or (base1 != 1 and n > 1):
             raise ValueError(f"base must be {out.dtype} {tuple(out.shape)} with contiguous rows on device {dev}")
-        bp, ldb = base.data_ptr(), base.stride(0)
-    ap = _ints("adapter", adapter, m, torch, dev)
+        bp = base.data_ptr()
+    if adapter.dtype is not torch.int32 or adapter.numel() != m or not adapter.is_contiguous() or adapter.get_device() != dev:
+        _ints("adapter", adapter, m, torch, dev)
     if ranks is not None:
-        rp = _ints("ranks", ranks, slots, torch, dev)
+        _ints("ranks", ranks, slots, torch, dev)
+        rp = ranks.data_ptr()
     if scales is not None:
-        if scales.dtype is not torch.float32 or scales.shape != (slots,) or not scales.is_contiguous() or scales.get_device() != dev:
+        if scales.dtype is not torch.float32 or scales.numel() != slots or not scales.is_contiguous() or scales.get_device() != dev:
             raise ValueError(f"scales must be a contiguous float32 [{slots}] on device {dev}")
         sp = scales.data_ptr()
     if work is not None:
         wp, wb = _scratch(work, dev)
-    packed = _LORA.pack(x.data_ptr(), x.stride(0), a.data_ptr(), b.data_ptr(), a0, b0, ap, rp, sp, bp, ldb, out.data_ptr(), out.stride(0),
+    packed = _LORA.pack(x.data_ptr(), x0, a.data_ptr(), b.data_ptr(), a0, b0, adapter.data_ptr(), rp, sp, bp, ldb, out.data_ptr(), o0,
                         TP_F32 if f32 else TP_BF16, m, n, k, r, slots, TP_ACT[act], 0, wp, wb)
-    _made(torch, current, here, call, packed, dev, stream)
+    s = current(dev) if stream is None else _stream_of(dev, stream)
+    status = call(packed, s) if s or here() == dev else _on_device(torch, call, packed, dev, s)
+    if status != TP_OK:
+        _check(lib(), status)
