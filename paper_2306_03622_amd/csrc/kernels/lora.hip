@@ -47,63 +47,72 @@ __device__ __forceinline__ uint4 first_of(uint4 v, int n) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-__device__ __forceinline__ float lora_act(float v, int act) {
-  if (act == ACT_RELU) return v < 0.f ? 0.f : v;      // keeps NaN
-  return act_apply(v, act);
-}
-
 __device__ __forceinline__ int rank_of(const Lora& a, int ad) { return a.ranks ? min(max(a.ranks[ad], 0), a.R) : a.R; }
 
 // The rest of t behind its bf16 part (none behind an infinity or NaN).
 __device__ __forceinline__ float rest_of(float t, uint16_t part) { return fabsf(t) < INFINITY ? t - bf2f(part) : 0.f; }
 
-// Four outputs of a row from n on: the base's values, loaded ahead where they come in one piece, and the rest.
+// The base's four values of a row from output n on, loaded ahead (m: a row that is there, n: any output; those behind N are not used).
 template <bool F32>
-struct Run {
+struct Base {
   uint4 w;                // fp32, or bf16 pairs in x and y
-  // (m: a row that is there, n: any output; what is not stored is not used)
   __device__ __forceinline__ void load(const Lora& a, bool vec, int64_t m, int n) {
     w = zeros();
-    if (!a.base || !vec || n + 4 > a.N) return;
-    const char* p = static_cast<const char*>(a.base) + (m * a.ldbase + n) * (F32 ? 4 : 2);
+    if (!a.base || n >= a.N) return;
+    const int64_t at = m * a.ldbase + n;
     if constexpr (F32) {
-      w = load16(p);
+      const uint32_t* p = static_cast<const uint32_t*>(a.base) + at;
+      if (vec) {
+        w = load16(p);
+      } else {
+        const int last = a.N - 1 - n;               // the last one again behind N
+        w = make_uint4(p[0], p[min(1, last)], p[min(2, last)], p[min(3, last)]);
+      }
     } else {
-      const uint2 u = *reinterpret_cast<const uint2*>(p);
-      w.x = u.x, w.y = u.y;
+      const uint16_t* p = static_cast<const uint16_t*>(a.base) + at;
+      if (vec) {
+        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        w.x = u.x, w.y = u.y;
+      } else {
+        const int last = a.N - 1 - n;
+        w.x = p[0] | (uint32_t)p[min(1, last)] << 16, w.y = p[min(2, last)] | (uint32_t)p[min(3, last)] << 16;
+      }
     }
   }
-  // base + v, activation, rounding
-  __device__ __forceinline__ void finish(const Lora& a, bool vec, int64_t m, int n, f32x4 v) const {
-    if (n >= a.N) return;
-    if (vec && n + 4 <= a.N) {
-      char* p = static_cast<char*>(a.y) + (m * a.ldy + n) * (F32 ? 4 : 2);
-      if constexpr (F32) {
-        v += __builtin_bit_cast(f32x4, w);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = lora_act(v[i], a.act);
-        *reinterpret_cast<f32x4*>(p) = v;
-      } else {
-        v += f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = lora_act(v[i], a.act);
-        *reinterpret_cast<uint2*>(p) = make_uint2(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]));
-      }
-      return;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (n + j >= a.N) continue;
-      if constexpr (F32) {
-        const float base = a.base ? static_cast<const float*>(a.base)[m * a.ldbase + n + j] : 0.f;
-        static_cast<float*>(a.y)[m * a.ldy + n + j] = lora_act(v[j] + base, a.act);
-      } else {
-        const float base = a.base ? bf2f(static_cast<const uint16_t*>(a.base)[m * a.ldbase + n + j]) : 0.f;
-        static_cast<uint16_t*>(a.y)[m * a.ldy + n + j] = f2bf(lora_act(v[j] + base, a.act));
-      }
-    }
+  __device__ __forceinline__ f32x4 values() const {
+    if constexpr (F32) return __builtin_bit_cast(f32x4, w);
+    return f32x4{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xffff0000u), __uint_as_float(w.y << 16), __uint_as_float(w.y & 0xffff0000u)};
   }
 };
+
+// The activation of all of a lane's results: one choice for them, so that their chains of operations overlap.
+template <int R>
+__device__ __forceinline__ void activate(f32x4 (&v)[R], int act) {
+  if (act == ACT_RELU) {
+#pragma unroll
+    for (int i = 0; i < 4 * R; ++i) v[i / 4][i % 4] = v[i / 4][i % 4] < 0.f ? 0.f : v[i / 4][i % 4];           // keeps NaN
+  } else if (act == ACT_GELU) {
+#pragma unroll
+    for (int i = 0; i < 4 * R; ++i) v[i / 4][i % 4] = act_apply(v[i / 4][i % 4], ACT_GELU);
+  }
+}
+
+// Four outputs of row m from n on.
+template <bool F32>
+__device__ __forceinline__ void store(const Lora& a, bool vec, int64_t m, int n, f32x4 v) {
+  const int64_t at = m * a.ldy + n;
+  if (vec && n < a.N) {
+    if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at) = v;
+    else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + at) = make_uint2(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]));
+    return;
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (n + j >= a.N) continue;
+    if constexpr (F32) static_cast<float*>(a.y)[at + j] = v[j];
+    else static_cast<uint16_t*>(a.y)[at + j] = f2bf(v[j]);
+  }
+}
 
 // The adapter of row m0 + lane (lanes below ROWS), -1: none.
 template <int ROWS>
@@ -312,10 +321,10 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
         *reinterpret_cast<uint4*>(to + at_of(16 * (row & 3) + (row >> 2), ch)) = first_of(bw[i], rank - 8 * ch);
       }
     };
-    Run<F32> run[4];
+    Base<F32> base[4];
     auto load_base = [&](int nb) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) run[i].load(a, g.vec, m[i], nb * 64 + 4 * r16);
+      for (int i = 0; i < 4; ++i) base[i].load(a, g.vec, m[i], nb * 64 + 4 * r16);
     };
     // everything that is read goes under way before anything is waited for, the rank among it
     if (ad >= 0) load_b(nb0);
@@ -377,15 +386,18 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
               for (int p = 0; p < PARTS; ++p) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(tf[rc][p]), bf, acc[e], 0, 0, 0);
             }
           }
-        Run<F32> now[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) now[i] = run[i];
-        if (nb + 1 < nb1) load_base(nb + 1);
         // lane holds outputs 64 nb + 4 r16 + e of rows 4 q4 + i
+        f32x4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          v[i] = base[i].values();
+          if (with[i]) v[i] += f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+        }
+        if (nb + 1 < nb1) load_base(nb + 1);
+        activate(v, a.act);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (first + 4 * q4 + i < count)
-            now[i].finish(a, g.vec, m[i], nb * 64 + 4 * r16, with[i] ? f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]} : f32x4{0, 0, 0, 0});
+          if (first + 4 * q4 + i < count) store<F32>(a, g.vec, m[i], nb * 64 + 4 * r16, v[i]);
       }
       if (rank && nb + 1 < nb1) {
         keep_b(lds[(nb + 1 - nb0) & 1], rank);
@@ -497,14 +509,17 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
     }
   }
   // lane holds outputs n0 + 4 r16 + e of rows 4 q4 + i
+  f32x4 v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int to = m0 + 4 * q4 + i;
-    if (to >= a.M) continue;
-    Run<F32> run;
-    run.load(a, g.vec, to, n0 + 4 * r16);
-    run.finish(a, g.vec, to, n0 + 4 * r16, f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]});
+    Base<F32> base;
+    base.load(a, g.vec, min(m0 + 4 * q4 + i, a.M - 1), n0 + 4 * r16);
+    v[i] = base.values() + f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
   }
+  activate(v, a.act);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (m0 + 4 * q4 + i < a.M) store<F32>(a, g.vec, m0 + 4 * q4 + i, n0 + 4 * r16, v[i]);
 }
 
 template <bool F32>
@@ -527,7 +542,7 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   g.t = sp.partials;
   g.tiles_n = (int)(((int64_t)a.N + 255) / 256);
   const uintptr_t four = a.f32 ? 16 : 8;
-  g.vec = (uintptr_t)a.y % four == 0 && a.ldy % 4 == 0 && (uintptr_t)a.base % four == 0 && a.ldbase % 4 == 0;
+  g.vec = a.N % 4 == 0 && (uintptr_t)a.y % four == 0 && a.ldy % 4 == 0 && (uintptr_t)a.base % four == 0 && a.ldbase % 4 == 0;
   if (((int64_t)a.M + 15) / 16 * g.tiles_n >= 1 << 24) return hipErrorInvalidValue;
   const LoraPlan p = lora_plan(a.M, a.N, a.K, a.R, a.adapters, sp.partials ? sp.partial_bytes : 0);
   if (p.splits == 0)

@@ -26,7 +26,7 @@ inline LoraPlan lora_plan(int64_t M, int64_t N, int64_t K, int64_t R, int64_t ad
   const int64_t ds = std::max<int64_t>(1, std::min<int64_t>({adapters, 32, M, std::max<int64_t>(2, 512 / tiles)}));
   const int64_t z = std::max<int64_t>(1, std::min<int64_t>({K / 512, 8, 512 / (tiles * ds), fits}));
   const int64_t jobs = (M + 63) / 64;
-  const int64_t run = std::max<int64_t>(1, std::min<int64_t>(8, jobs * blocks / 2048));
+  const int64_t run = std::max<int64_t>(1, std::min<int64_t>(8, jobs * blocks / 1024));
   const int64_t wgs = jobs * ((blocks + run - 1) / run);
   const int64_t us = std::max<int64_t>(1, std::min<int64_t>({adapters, 64, M, std::max<int64_t>(2, 4096 / wgs)}));
   return {(int)z, (int)ds, (int)us, (int)run};
