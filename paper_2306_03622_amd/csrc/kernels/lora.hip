@@ -5,6 +5,7 @@
 // rows, finds the adapters that they name (the rows' numbers lie one in a lane; a ballot gives an adapter's rows), and takes
 // the rows of one adapter together, in blocks of 16, wherever in the tile they stand: rows of many requests in any order need no
 // sorting, and no row meets another's adapter. Where there are few tiles, the adapters of a tile go to several workgroups.
+// Where many tiles could hold many adapters each, k_lora_order first writes down the rows adapter by adapter, and tiles are of that order.
 // Without scratch k_lora does both in one launch and computes t anew for every 256 outputs.
 //
 // t is taken as bf16 parts (two, three for fp32 results: 2^-16 and 2^-24 of t), all multiplied by B, whose values are bf16 as they are.
@@ -19,6 +20,7 @@ namespace k {
 struct LoraArgs {
   Lora a;
   float* t;               // [splits][M][R]
+  int2* order;            // [M] rows and their adapters (-1: none), adapter by adapter; NULL: as they stand
   int splits;             // over K
   int slots;              // workgroups (or waves) that share a tile's adapters
   int tiles_n;            // blocks of outputs
@@ -31,6 +33,7 @@ struct PtrFields<LoraArgs> {
   static void add(std::vector<uint32_t>& v, uint32_t at) {
     PtrFields<Lora>::add(v, at + (uint32_t)offsetof(LoraArgs, a));
     v.push_back(at + (uint32_t)offsetof(LoraArgs, t));
+    v.push_back(at + (uint32_t)offsetof(LoraArgs, order));
   }
 };
 
@@ -52,7 +55,8 @@ __device__ __forceinline__ int rank_of(const Lora& a, int ad) { return a.ranks ?
 // The rest of t behind its bf16 part (none behind an infinity or NaN).
 __device__ __forceinline__ float rest_of(float t, uint16_t part) { return fabsf(t) < INFINITY ? t - bf2f(part) : 0.f; }
 
-// The base's four values of a row from output n on, loaded ahead (m: a row that is there, n: any output; those behind N are not used).
+// A lane's four outputs of a row: n, n + 1, .. where rows are vectors of four (vec), else n, n + 16, .. so that 16 lanes' are side by side.
+// The base's values there, loaded ahead (m: a row that is there; outputs behind N are not used).
 template <bool F32>
 struct Base {
   uint4 w;                // fp32, or bf16 pairs in x and y
@@ -66,7 +70,7 @@ struct Base {
         w = load16(p);
       } else {
         const int last = a.N - 1 - n;               // the last one again behind N
-        w = make_uint4(p[0], p[min(1, last)], p[min(2, last)], p[min(3, last)]);
+        w = make_uint4(p[0], p[min(16, last)], p[min(32, last)], p[min(48, last)]);
       }
     } else {
       const uint16_t* p = static_cast<const uint16_t*>(a.base) + at;
@@ -75,7 +79,7 @@ struct Base {
         w.x = u.x, w.y = u.y;
       } else {
         const int last = a.N - 1 - n;
-        w.x = p[0] | (uint32_t)p[min(1, last)] << 16, w.y = p[min(2, last)] | (uint32_t)p[min(3, last)] << 16;
+        w.x = p[0] | (uint32_t)p[min(16, last)] << 16, w.y = p[min(32, last)] | (uint32_t)p[min(48, last)] << 16;
       }
     }
   }
@@ -97,7 +101,7 @@ __device__ __forceinline__ void activate(f32x4 (&v)[R], int act) {
   }
 }
 
-// Four outputs of row m from n on.
+// Row m's four outputs.
 template <bool F32>
 __device__ __forceinline__ void store(const Lora& a, bool vec, int64_t m, int n, f32x4 v) {
   const int64_t at = m * a.ldy + n;
@@ -108,17 +112,26 @@ __device__ __forceinline__ void store(const Lora& a, bool vec, int64_t m, int n,
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    if (n + j >= a.N) continue;
-    if constexpr (F32) static_cast<float*>(a.y)[at + j] = v[j];
-    else static_cast<uint16_t*>(a.y)[at + j] = f2bf(v[j]);
+    if (n + 16 * j >= a.N) continue;
+    if constexpr (F32) static_cast<float*>(a.y)[at + 16 * j] = v[j];
+    else static_cast<uint16_t*>(a.y)[at + 16 * j] = f2bf(v[j]);
   }
 }
 
-// The adapter of row m0 + lane (lanes below ROWS), -1: none.
-template <int ROWS>
-__device__ __forceinline__ int adapter_at(const Lora& a, int m0, int lane) {
-  const int id = lane < ROWS && m0 + lane < a.M ? a.adapter[m0 + lane] : -1;
+__device__ __forceinline__ int adapter_of(const Lora& a, int row) {
+  const int id = a.adapter[row];
   return (unsigned)id < (unsigned)a.adapters ? id : -1;
+}
+
+// The row at place m0 + lane of a tile of ROWS (lanes behind it, and places behind the last: row m0) and its adapter (-1: none).
+template <int ROWS>
+__device__ __forceinline__ int2 place_of(const LoraArgs& g, int m0, int lane) {
+  const bool real = lane < ROWS && m0 + lane < g.a.M;
+  if (g.order) {
+    const int2 p = g.order[real ? m0 + lane : m0];
+    return make_int2(p.x, real ? p.y : -1);
+  }
+  return make_int2(real ? m0 + lane : m0, real ? adapter_of(g.a, m0 + lane) : -1);
 }
 
 // Lane j holds the number of the j-th set bit of `mask` (behind the last: 0).
@@ -126,6 +139,49 @@ __device__ __forceinline__ int nth_of(unsigned long long mask, int lane) {
   const int before = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
   // lanes without a bit send to lane 63, where the last bit's lane sends too if all 64 are set: then no lane is without
   return __builtin_amdgcn_ds_permute((mask >> lane & 1 ? before : 63) * 4, mask >> lane & 1 ? lane : 0);
+}
+
+// The rows adapter by adapter, those without one last: counted, summed up, and put in their places (in no fixed order inside an
+// adapter: a row's result does not depend on its place). One workgroup: 8192 rows take 5 us.
+constexpr int kMostBins = 4096;
+
+__global__ __launch_bounds__(1024) void k_lora_order(LoraArgs g) {
+  __shared__ int bins[kMostBins], sums[1024];
+  const Lora& a = g.a;
+  const int tid = threadIdx.x, n = a.adapters + 1;
+  for (int i = tid; i < n; i += 1024) bins[i] = 0;
+  __syncthreads();
+  for (int m = tid; m < a.M; m += 1024) {
+    const int id = adapter_of(a, m);
+    atomicAdd(&bins[id < 0 ? n - 1 : id], 1);
+  }
+  __syncthreads();
+  // each thread's four bins, then the threads
+  int mine[kMostBins / 1024], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kMostBins / 1024; ++i) {
+    const int at = tid * (kMostBins / 1024) + i;
+    mine[i] = sum;
+    sum += at < n ? bins[at] : 0;
+  }
+  sums[tid] = sum;
+  __syncthreads();
+  for (int step = 1; step < 1024; step *= 2) {
+    const int before = tid >= step ? sums[tid - step] : 0;
+    __syncthreads();
+    sums[tid] += before;
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < kMostBins / 1024; ++i) {
+    const int at = tid * (kMostBins / 1024) + i;
+    if (at < n) bins[at] = sums[tid] - sum + mine[i];
+  }
+  __syncthreads();
+  for (int m = tid; m < a.M; m += 1024) {
+    const int id = adapter_of(a, m);
+    g.order[atomicAdd(&bins[id < 0 ? n - 1 : id], 1)] = make_int2(m, id);
+  }
 }
 
 // Workgroups are handed out to the eight XCDs in turn: tiles side by side, whose rows often have the same adapter, for one XCD.
@@ -162,7 +218,8 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
   at /= g.splits;
   // slots last: the others' workgroups may have nothing to do
   const int tiles = (a.M + 31) / 32, slot = at / tiles, m0 = tile_of(at % tiles, tiles) * 32;
-  const int mine = adapter_at<32>(a, m0, lane);
+  const int2 place = place_of<32>(g, m0, lane);
+  const int mine = place.y;
   const int full = a.K >> 6, stride = g.splits * W, s0 = z * W + wave, n = full > s0 ? (full - s0 + stride - 1) / stride : 0;
   const char* ring = lds + wave * RING;
   const uint32_t ring0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * RING;
@@ -175,7 +232,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
 #pragma unroll
     for (int i = 0; i < LPS; ++i) {
       const int r = 8 * i + (lane >> 3), j = r - 16 * MB, ch = (lane & 7) ^ key_of(r);
-      const int row = m0 + __shfl(rows, i < 2 * MB && r < count ? r : 0, 64);
+      const int row = __shfl(rows, i < 2 * MB && r < count ? r : 0, 64);
       from[i] = (i < 2 * MB ? a.x + row * a.ldx : xa + (int64_t)min(j, a.R - 1) * a.K) + 8 * ch;
     }
     f32x4 d[RB][MB];
@@ -230,7 +287,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
         uint4 xf[MB], af[RB];
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb) {
-          const int j = mb * 16 + r16, row = m0 + __shfl(rows, j < count ? j : 0, 64);
+          const int j = mb * 16 + r16, row = __shfl(rows, j < count ? j : 0, 64);
           xf[mb] = in ? load16(a.x + row * a.ldx + k) : zeros();
         }
 #pragma unroll
@@ -254,7 +311,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
 #pragma unroll
         for (int w = 0; w < W; ++w) t += part[w][i % 16][j];
         const int row = __shfl(rows, min(j, 31), 64);
-        if (j < count && r < a.R) g.t[((int64_t)z * a.M + m0 + row) * a.R + r] = r < rank ? t * scale : 0.f;
+        if (j < count && r < a.R) g.t[((int64_t)z * a.M + row) * a.R + r] = r < rank ? t * scale : 0.f;
       }
     }
     __syncthreads();
@@ -265,7 +322,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
     const unsigned long long mask = __ballot(mine == ad);
     left &= ~mask;
     if (j % g.slots != slot) continue;
-    const int rows = nth_of(mask, lane), count = __builtin_popcountll(mask);
+    const int rows = __shfl(place.x, nth_of(mask, lane), 64), count = __builtin_popcountll(mask);
     if (count > 16) body(std::integral_constant<int, 2>(), ad, rows, count);
     else body(std::integral_constant<int, 1>(), ad, rows, count);
   }
@@ -273,9 +330,10 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
 
 // y of the rows of 64 that name an adapter of this slot (and in slot 0 those without one), g.run blocks of 64 outputs. The rows of one
 // adapter go to the waves, 16 to each; the parts of t stay in registers. A block of B (64 rows, in memory as they lie) goes through
-// registers into LDS, two blocks in turn, so that the next one's values and base are under way while one is computed. Output n
-// = 64 nb + 4 l + e comes from lane l and block e: a lane has four consecutive outputs of four rows, 16 lanes a row's 64. In
-// LDS row 16 e + l holds B's row 4 l + e, its chunks moved by at_of so that 16 rows' same chunk falls on different banks.
+// registers into LDS, two blocks in turn, so that the next one's values and base are under way while one is computed. Product e's 16
+// lanes of outputs are n = 64 nb + 4 l + e: a lane has four consecutive outputs of four rows, 16 lanes a row's 64 (16 e + l where rows
+// are no vectors of four). In LDS row 16 e + l holds that row of B, its chunks moved by at_of so that 16 rows' same chunk falls on
+// different banks.
 template <bool F32, int RC>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
   constexpr int W = 4, PARTS = F32 ? 3 : 2, ROWS = 16 * W, PITCH = 64 * RC, CPR = 4 * RC, MINE = CPR / W;
@@ -290,7 +348,8 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
   if (tile >= tiles) return;
   const int m0 = tile * ROWS, nb0 = part * g.run, nb1 = min(nb0 + g.run, (a.N + 63) / 64);
   auto at_of = [](int row, int ch) { return row * PITCH + ((ch ^ (RC == 1 ? row >> 2 & 3 : RC == 2 ? row >> 1 & 7 : row & 15)) << 4); };
-  const int mine = adapter_at<ROWS>(a, m0, lane);
+  const int2 place = place_of<ROWS>(g, m0, lane);
+  const int mine = place.y, lane_n = g.vec ? 4 * r16 : r16;
 
   // the rows whose bits are set in `mask`: of adapter ad (-1: none), or of none
   auto body = [&](int ad, unsigned long long mask) __attribute__((always_inline)) {
@@ -302,7 +361,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int at = first + 4 * q4 + i, row = __shfl(list, at < count ? at : 0, 64);
-      m[i] = m0 + row;
+      m[i] = __shfl(place.x, row, 64);
       with[i] = __shfl(mine, row, 64) >= 0;
     }
     // this lane's chunks of a block of B: read as far as R (what lies behind the rank is dropped below), the last row again behind N
@@ -318,22 +377,22 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
 #pragma unroll
       for (int i = 0; i < MINE; ++i) {
         const int at = i * 64 * W + tid, row = at / CPR, ch = at % CPR;
-        *reinterpret_cast<uint4*>(to + at_of(16 * (row & 3) + (row >> 2), ch)) = first_of(bw[i], rank - 8 * ch);
+        *reinterpret_cast<uint4*>(to + at_of(g.vec ? 16 * (row & 3) + (row >> 2) : row, ch)) = first_of(bw[i], rank - 8 * ch);
       }
     };
     Base<F32> base[4];
     auto load_base = [&](int nb) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) base[i].load(a, g.vec, m[i], nb * 64 + 4 * r16);
+      for (int i = 0; i < 4; ++i) base[i].load(a, g.vec, m[i], nb * 64 + lane_n);
     };
     // everything that is read goes under way before anything is waited for, the rank among it
     if (ad >= 0) load_b(nb0);
     if (busy) load_base(nb0);
-    const int row = __shfl(list, first + r16 < count ? first + r16 : 0, 64);
-    const bool has = __shfl(mine, row, 64) >= 0;
+    const int at = __shfl(list, first + r16 < count ? first + r16 : 0, 64), row = __shfl(place.x, at, 64);
+    const bool has = __shfl(mine, at, 64) >= 0;
     f32x4 tv[RC][2];
     auto load_t = [&](int z, int rc, int i) __attribute__((always_inline)) {
-      return *reinterpret_cast<const f32x4*>(g.t + ((int64_t)z * a.M + m0 + row) * a.R + min(rc * 32 + 8 * q4, a.R - 8) + 4 * i);
+      return *reinterpret_cast<const f32x4*>(g.t + ((int64_t)z * a.M + row) * a.R + min(rc * 32 + 8 * q4, a.R - 8) + 4 * i);
     };
 #pragma unroll
     for (int rc = 0; rc < RC; ++rc)
@@ -386,7 +445,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
               for (int p = 0; p < PARTS; ++p) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(tf[rc][p]), bf, acc[e], 0, 0, 0);
             }
           }
-        // lane holds outputs 64 nb + 4 r16 + e of rows 4 q4 + i
+        // lane holds its outputs of rows 4 q4 + i
         f32x4 v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -397,7 +456,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
         activate(v, a.act);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (first + 4 * q4 + i < count) store<F32>(a, g.vec, m[i], nb * 64 + 4 * r16, v[i]);
+          if (first + 4 * q4 + i < count) store<F32>(a, g.vec, m[i], nb * 64 + lane_n, v[i]);
       }
       if (rank && nb + 1 < nb1) {
         keep_b(lds[(nb + 1 - nb0) & 1], rank);
@@ -432,7 +491,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
   const int m0 = (int)(blockIdx.x / g.tiles_n) * 16, n0 = ((int)(blockIdx.x % g.tiles_n) * kWaves + wave) * 64;
   const int m = m0 + r16;
   const bool row = m < a.M;
-  const int mine = __shfl(adapter_at<16>(a, m0, lane), r16, 64);
+  const int mine = row ? adapter_of(a, m) : -1;
   const uint16_t* x = a.x + (row ? m : m0) * a.ldx;
 
   f32x4 acc[4];
@@ -495,7 +554,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
       for (int p = 0; p < PARTS; ++p) tf[p] = as_bf16x8(load16(&ts[p][r16][r]));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int n = n0 + 4 * r16 + e;
+        const int n = n0 + (g.vec ? 4 * r16 + e : 16 * e + r16);
         const uint4 bf = n < a.N && r < rank ? first_of(load16(up + (int64_t)n * a.R + r), rank - r) : zeros();
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) y[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tf[p], as_bf16x8(bf), y[e], 0, 0, 0);
@@ -508,18 +567,18 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
       for (int e = 0; e < 4; ++e) acc[e][i] = y[e][i];
     }
   }
-  // lane holds outputs n0 + 4 r16 + e of rows 4 q4 + i
+  // lane holds its outputs of rows 4 q4 + i
   f32x4 v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     Base<F32> base;
-    base.load(a, g.vec, min(m0 + 4 * q4 + i, a.M - 1), n0 + 4 * r16);
+    base.load(a, g.vec, min(m0 + 4 * q4 + i, a.M - 1), n0 + (g.vec ? 4 * r16 : r16));
     v[i] = base.values() + f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
   }
   activate(v, a.act);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (m0 + 4 * q4 + i < a.M) store<F32>(a, g.vec, m0 + 4 * q4 + i, n0 + 4 * r16, v[i]);
+    if (m0 + 4 * q4 + i < a.M) store<F32>(a, g.vec, m0 + 4 * q4 + i, n0 + (g.vec ? 4 * r16 : r16), v[i]);
 }
 
 template <bool F32>
@@ -548,6 +607,11 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   if (p.splits == 0)
     return launch(a.f32 ? k_lora<true> : k_lora<false>, dim3((unsigned)((a.M + 15) / 16 * g.tiles_n)), dim3(64 * kWaves), 0, s, g);
   g.splits = p.splits;
+  if (p.order) {
+    g.order = reinterpret_cast<int2*>(g.t + (int64_t)p.splits * a.M * a.R);       // (R is even: at 8 bytes)
+    const hipError_t e = launch(k_lora_order, dim3(1), dim3(1024), 0, s, g);
+    if (e != hipSuccess) return e;
+  }
   g.slots = p.down_slots;
   const unsigned tiles = (a.M + 31) / 32;
   const int rb = (a.R + 15) / 16;
