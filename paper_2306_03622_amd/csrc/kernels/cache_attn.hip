@@ -122,9 +122,28 @@ __global__ __launch_bounds__(64 * W) void k_cache_attention(CacheAttnArgs g) {
   const int z = id % g.splits, rt = id / g.splits;
   const int hk = bh % c.heads, b = bh / c.heads;
 
+  // What does not wait for the lengths is asked for beside them: Q's rows (the last one again where there is none; a row that has
+  // no query is computed and not stored) and, for keys from the first on, the pages of this wave's first tiles.
+  const int row0 = rt * 16 * RB, all = a.p.q_len * g.share;
+  bf16x8 qf[RB][DC];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = min(row0 + rb * 16 + r16, all - 1), qi = row / g.share, qh = hk * g.share + row - qi * g.share;
+    const uint16_t* p = a.q + b * a.qs[0] + qi * a.qs[1] + qh * a.qs[2];
+#pragma unroll
+    for (int i = 0; i < DC; ++i)      // e4m3 keys come 16 columns a lane, for two products
+      qf[rb][i] = as_bf16x8(*reinterpret_cast<const uint4*>(p + (E4M3 ? 64 * (i / 2) + 16 * q4 + 8 * (i % 2) : 32 * i + 8 * q4)));
+  }
+  const auto* table = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.p.table + b * a.p.table_stride);
+  auto page_at = [&](int t, int hb) __attribute__((always_inline)) { return table[min((t * 32 + hb * 16) >> c.lg, a.p.max_pages - 1)]; };
+  const bool from0 = a.window < 0 && g.splits == 1;
+  int early[NST - 1][2];
+#pragma unroll
+  for (int i = 0; i < NST - 1; ++i)
+#pragma unroll
+    for (int hb = 0; hb < 2; ++hb) early[i][hb] = page_at(wave + i * W, hb);
   const Lens len = lens_of(a.p, b);
-  const int qn = len.qn, kn = min(len.kn, a.kv_len);
-  const int rows = qn * g.share, row0 = rt * 16 * RB, all = a.p.q_len * g.share;
+  const int qn = len.qn, kn = min(len.kn, a.kv_len), rows = qn * g.share;
   if (row0 >= rows) return;
   const int shift = kn - qn;                        // query i stands at i + shift
   const int row1 = min(row0 + 16 * RB, rows) - 1;
@@ -135,35 +154,25 @@ __global__ __launch_bounds__(64 * W) void k_cache_attention(CacheAttnArgs g) {
   const int t0 = (int)((int64_t)n * z / g.splits), t1 = (int)((int64_t)n * (z + 1) / g.splits);
   auto tile = [&](int t) __attribute__((always_inline)) { return t < ns ? t : w0 + t - ns; };
 
-  // this lane's rows of Q (the last one again where there is none) and what they see
-  bf16x8 qf[RB][DC];
-  Seen me[RB];
+  Seen me[RB];                                      // what this lane's rows see
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int row = min(row0 + rb * 16 + r16, rows - 1), qi = row / g.share, qh = hk * g.share + row - qi * g.share;
-    me[rb] = seen_at(a, qi + shift, kn);
-    const uint16_t* p = a.q + b * a.qs[0] + qi * a.qs[1] + qh * a.qs[2];
-#pragma unroll
-    for (int i = 0; i < DC; ++i)      // e4m3 keys come 16 columns a lane, for two products
-      qf[rb][i] = as_bf16x8(*reinterpret_cast<const uint4*>(p + (E4M3 ? 64 * (i / 2) + 16 * q4 + 8 * (i % 2) : 32 * i + 8 * q4)));
-  }
+  for (int rb = 0; rb < RB; ++rb) me[rb] = seen_at(a, min(row0 + rb * 16 + r16, rows - 1) / g.share + shift, kn);
 
   char* ring = lds + wave * RING;
   const uint32_t ring0 = (uint32_t)(uintptr_t)LDS_PTR(char, lds) + wave * RING;
-  const auto* table = (const __attribute__((address_space(4))) int32_t*)(uintptr_t)(a.p.table + b * a.p.table_stride);
   const char *kp = static_cast<const char*>(c.k) + hk * c.ks[2], *vp = static_cast<const char*>(c.v) + hk * c.vs[2];
   const int mask = (1 << c.lg) - 1;
   uint32_t gone = 0;                                // two bits a stage under way, the youngest lowest: halves in no page
   const int lr = lane / T::CPR, lc = lane % T::CPR;
-  // Loads tile `t` into a slot: K's halves, V's halves, exponents.
-  auto issue = [&](int slot, int t) __attribute__((always_inline)) {
+  // Loads tile `t`, in these pages, into a slot: K's halves, V's halves, exponents.
+  auto issue = [&](int slot, int t, int page0, int page1) __attribute__((always_inline)) {
     const uint32_t dst = ring0 + slot * T::SBYTES;
     uint32_t xoff[2];
     gone <<= 2;
 #pragma unroll
     for (int hb = 0; hb < 2; ++hb) {
       const int key = __builtin_amdgcn_readfirstlane(t * 32 + hb * 16), at = key & mask;
-      int page = table[min(key >> c.lg, a.p.max_pages - 1)];
+      int page = hb ? page1 : page0;
       const bool ok = (unsigned)page < (unsigned)c.pages && key >> c.lg < a.p.max_pages;
       const int rows = ok ? min(max(kn - key, 0), 16) : 0;
       page = ok ? page : 0;
@@ -364,7 +373,7 @@ __global__ __launch_bounds__(64 * W) void k_cache_attention(CacheAttnArgs g) {
   auto mine_at = [&](int i) __attribute__((always_inline)) { return tile(t0 + wave + i * W); };
 #pragma unroll
   for (int i = 0; i < NST - 1; ++i)
-    if (i < mine) issue(i, mine_at(i));
+    if (i < mine) issue(i, mine_at(i), from0 ? early[i][0] : page_at(mine_at(i), 0), from0 ? early[i][1] : page_at(mine_at(i), 1));
   // the queries have arrived: else the compiler, which does not count the loads to LDS, waits for them in the loop
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb)
@@ -375,7 +384,8 @@ __global__ __launch_bounds__(64 * W) void k_cache_attention(CacheAttnArgs g) {
     reads_done();
     uint32_t lost;
     if (i + NST - 1 < mine) {
-      issue(slot == 0 ? NST - 1 : slot - 1, mine_at(i + NST - 1));
+      const int t = mine_at(i + NST - 1);
+      issue(slot == 0 ? NST - 1 : slot - 1, t, page_at(t, 0), page_at(t, 1));
       loads_left<(NST - 1) * T::LPS>();
       lost = gone >> (2 * (NST - 1)) & 3;
     } else {
@@ -520,8 +530,10 @@ hipError_t go(CacheAttnArgs g, hipStream_t s) {
 }
 
 template <int D, bool E4M3>
-hipError_t by_rows(const CacheAttnArgs& g, int rb, hipStream_t s) {
+hipError_t by_rows(const CacheAttnArgs& g, const CachePlan& plan, hipStream_t s) {
+  const int rb = plan.rb;
   constexpr int NST = D == 64 ? 3 : 2;
+  if (rb == 1 && plan.waves == 1) return go<D, E4M3, 1, 1, 2>(g, s);
   return rb == 1 ? go<D, E4M3, 1, 4, NST>(g, s) : rb == 2 ? go<D, E4M3, 2, 4, NST>(g, s) : go<D, E4M3, 4, 4, NST>(g, s);
 }
 
@@ -542,8 +554,8 @@ hipError_t cache_attention(const CacheAttention& a, const Split& sp, hipStream_t
   const CachePlan plan = cache_plan(c.dim, c.e4m3, rows, heads, span, a.p.batch == 1 || span <= a.kv_len / 2, sp.partials ? sp.partial_bytes : 0);
   g.splits = plan.splits;
   g.part = sp.partials;
-  if (c.dim == 64) return c.e4m3 ? by_rows<64, true>(g, plan.rb, s) : by_rows<64, false>(g, plan.rb, s);
-  return c.e4m3 ? by_rows<128, true>(g, plan.rb, s) : by_rows<128, false>(g, plan.rb, s);
+  if (c.dim == 64) return c.e4m3 ? by_rows<64, true>(g, plan, s) : by_rows<64, false>(g, plan, s);
+  return c.e4m3 ? by_rows<128, true>(g, plan, s) : by_rows<128, false>(g, plan, s);
 }
 
 }  // namespace k

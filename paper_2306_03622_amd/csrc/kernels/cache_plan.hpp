@@ -7,7 +7,7 @@ namespace tp {
 namespace k {
 
 struct CachePlan {
-  int rb, splits;         // blocks of 16 rows a workgroup takes, workgroups over the keys
+  int rb, waves, splits;  // blocks of 16 rows a workgroup takes, its waves over the keys, workgroups over the keys
 };
 
 // Keys that a workgroup walks, about. window: negative: none.
@@ -38,7 +38,7 @@ inline CachePlan cache_plan(int dim, bool e4m3, int64_t rows, int64_t heads, int
     if (s > 1) t += 3000 + part * s / 5000;
     if (s == 1 || t < best) best = t, splits = (int)s;
   }
-  return {rb, splits};
+  return {rb, rb == 1 && span <= 64 ? 1 : 4, splits};
 }
 
 }  // namespace k
