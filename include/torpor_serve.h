@@ -49,11 +49,12 @@ typedef struct {
 
 /* Rows of keys and values, bf16, in and out of the cache: strides in elements between sequences, rows and heads, the values of a head
  * contiguous, at 16-byte boundaries (strides multiples of 8; those of a dimension of one entry are not used).
- * tps_cache_append writes rows i < q_lens[b] of k and v into the pages. Two rows of one call that stand for the same place leave
- * one of the two there, each head's values with their scale. Pages that it does not write are not touched.
+ * tps_cache_append writes rows i < q_lens[b] of k and v into the pages. Two rows of one call that stand for the same place (sequences
+ * that share the page they append to) leave a mixture of the two there. Pages that it does not write are not touched.
  * tps_cache_read writes rows i < q_lens[b] from the pages (q_lens = kv_lens: whole sequences); other rows are left
  * as they are. 8-bit values that a scale takes beyond bf16's range are infinities, those below it are rounded. Rows do
- * not overlap each other (when written) nor the cache. batch * q_len * kv_heads is below 2^26. */
+ * not overlap each other (when written) nor the cache. batch * q_len * kv_heads is below 2^26, batch *
+ * kv_heads below 2^22. */
 typedef struct {
   tps_cache cache;
   const int32_t* table;

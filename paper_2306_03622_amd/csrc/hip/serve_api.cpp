@@ -78,8 +78,8 @@ tp_status rows_call(const char* who, const tps_cache_rows_args* a, void* stream,
   if (const char* e = pages_of(a->table, a->table_stride, a->q_lens, a->kv_lens, a->batch, a->q_len, a->max_pages, &g.p)) return inval(who, e);
   if (!a->k || !a->v) return inval(who, "NULL buffer");
   if ((uintptr_t)a->k % 16 || (uintptr_t)a->v % 16) return inval(who, "k and v must start at 16-byte boundaries");
-  if ((int64_t)a->batch * a->q_len > ((1 << 26) - 1) / a->cache.kv_heads)
-    return inval(who, "batch * q_len * kv_heads must be below 2^26");
+  if ((int64_t)a->batch * a->q_len > ((1 << 26) - 1) / a->cache.kv_heads || (int64_t)a->batch * a->cache.kv_heads >= 1 << 22)
+    return inval(who, "batch * q_len * kv_heads must be below 2^26, batch * kv_heads below 2^22");
   const int64_t least = append ? 0 : a->cache.head_dim;
   if (const char* e = strides_of(a->k_stride, a->batch, a->q_len, a->cache.kv_heads, least, g.rks)) return inval(who, e);
   if (const char* e = strides_of(a->v_stride, a->batch, a->q_len, a->cache.kv_heads, least, g.rvs)) return inval(who, e);

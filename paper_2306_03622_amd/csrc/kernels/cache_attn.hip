@@ -534,6 +534,7 @@ hipError_t by_rows(const CacheAttnArgs& g, const CachePlan& plan, hipStream_t s)
   const int rb = plan.rb;
   constexpr int NST = D == 64 ? 3 : 2;
   if (rb == 1 && plan.waves == 1) return go<D, E4M3, 1, 1, 2>(g, s);
+  if (rb == 1 && plan.waves == 2) return go<D, E4M3, 1, 2, NST>(g, s);
   return rb == 1 ? go<D, E4M3, 1, 4, NST>(g, s) : rb == 2 ? go<D, E4M3, 2, 4, NST>(g, s) : go<D, E4M3, 4, 4, NST>(g, s);
 }
 

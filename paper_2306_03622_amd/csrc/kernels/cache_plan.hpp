@@ -20,25 +20,32 @@ inline int64_t cache_span(int64_t q_len, int64_t kv_len, int64_t window, int64_t
 inline CachePlan cache_plan(int dim, bool e4m3, int64_t rows, int64_t heads, int64_t span, bool even, uint64_t scratch) {
   const int rb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
   const int64_t wgs = (rows + 16 * rb - 1) / (16 * rb) * heads;
+  // one wave where the keys are two tiles at most (us, graph replay: 25 sequences of 12 key/value heads, up to 8 tokens 5.8, four waves 11.4)
+  if (rb == 1 && span <= 64) return {1, 1, 1};
   const int64_t fits = (int64_t)(scratch / 4) / (rows * heads * (dim + 2));
-  const int64_t most = std::min<int64_t>({64, span / 128, fits});
-  // Time by a model, in ns and bytes: a workgroup takes 3500 beside its keys, which come at 5400 for all, at most 30 (8 bits: 22) for one;
-  // 256 (8 bits: 512) run at once. Where lengths differ they are taken to be three quarters of the longest on average, short ones making
-  // room for the next. Partial results are written and read at 5000, and joined in 3000.
-  const double bytes = (double)span * 2 * dim * (e4m3 ? 1 : 2), part = (double)rows * heads * (dim + 2) * 8, one = e4m3 ? 22 : 30;
-  const int64_t once = e4m3 ? 512 : 256;
-  double best = 0;
-  int splits = 1;
-  for (int64_t s = 1; s <= std::max<int64_t>(1, most); ++s) {
-    const int64_t n = wgs * s;
-    const double each = bytes / s / std::min(one, 5400.0 / (double)std::min<int64_t>(once, n));
-    const double rounds = (double)((n + once - 1) / once);
-    double t = rounds * (3500 + each);
-    if (!even) t = std::max(3500 + bytes / s / one, rounds * 3500 + 0.75 * bytes * wgs / 5400 + 0.25 * each);
-    if (s > 1) t += 3000 + part * s / 5000;
-    if (s == 1 || t < best) best = t, splits = (int)s;
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({64, span / 128, fits, ((1 << 24) - 1) / wgs}));       // grids below 2^32 lanes
+  // Time by a model, in ns and bytes: a workgroup takes 3500 beside its keys, which come at 5400 for all, at most 7.5 (8 bits: 5.5) for
+  // a wave; on a CU run as many workgroups as its LDS holds. Where lengths differ they are taken to be three quarters of the longest on
+  // average, short ones making room for the next. Partial results are written and read at 5000, and joined in 3000. Of 20 shapes the
+  // choice was within 7% of the best of 22. Two waves instead of four (us): 32 / 8 heads of 128, 64 sequences of up to 128 / 256 / 500
+  // tokens 7.7 / 11.9 / 19.8 instead of 12.1 / 16.9 / 23.8, 8 of up to 300 8.5 instead of 6.9.
+  const double bytes = (double)span * 2 * dim * (e4m3 ? 1 : 2), part = (double)rows * heads * (dim + 2) * 8;
+  const int64_t ring = 64 * dim * (e4m3 ? 1 : 2) * (dim == 64 ? 3 : 2);       // a wave's (the exponents aside)
+  CachePlan best{rb, 4, 1};
+  double least = 0;
+  for (int waves = 4; waves >= (rb == 1 ? 2 : 4); waves -= 2) {
+    const int64_t once = 256 * std::max<int64_t>(1, 160 * 1024 / (ring * waves + 1024));
+    for (int64_t s = 1; s <= most; ++s) {
+      const int64_t n = wgs * s;
+      const double one = waves * (e4m3 ? 5.5 : 7.5), each = bytes / s / std::min(one, 5400.0 / (double)std::min<int64_t>(once, n));
+      const double rounds = (double)((n + once - 1) / once);
+      double t = rounds * (3500 + each);
+      if (!even) t = std::max(3500 + bytes / s / one, rounds * 3500 + 0.75 * bytes * wgs / 5400 + 0.25 * each);
+      if (s > 1) t += 3000 + part * s / 5000;
+      if (least == 0 || t < least) least = t, best = {rb, waves, (int)s};
+    }
   }
-  return {rb, rb == 1 && span <= 64 ? 1 : 4, splits};
+  return best;
 }
 
 }  // namespace k

@@ -113,7 +113,7 @@ BAD_PAGES = [{"table": None}, {"kv_lens": None}, {"table": 0x1002}, {"q_lens": 0
 @pytest.mark.parametrize("name", ["tps_cache_append", "tps_cache_read"])
 @pytest.mark.parametrize("kw", BAD_CACHE + BAD_PAGES + [
     {"k": None}, {"v": None}, {"k": 0x4008}, {"v": 0x5002}, {"k_stride": (384, 128, 60)}, {"v_stride": (384, -8, 64)}, {"k_stride": (1 << 41, 128, 64)},
-    {"batch": 1 << 13, "q_len": 1 << 12}, {"batch": 2 ** 31 - 1, "q_len": 2 ** 31 - 1}, {"reserved": 3}])
+    {"batch": 1 << 13, "q_len": 1 << 12}, {"batch": 2 ** 31 - 1, "q_len": 2 ** 31 - 1}, {"batch": 1 << 21, "q_len": 1}, {"reserved": 3}])
 def test_row_refusals(name, kw):
     st, msg = _status(name, rows_args(**kw))
     assert st == tp.TP_E_INVAL and msg.startswith(name + ": "), (st, msg)
