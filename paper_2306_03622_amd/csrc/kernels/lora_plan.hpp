@@ -24,7 +24,7 @@ inline LoraPlan lora_plan(int64_t M, int64_t N, int64_t K, int64_t R, int64_t ad
   // there: 64 rows of 8, 768 x 768, rank 8 26 / 8.5.
   if (std::min(M, adapters) == 1 && K * ((R + 15) / 16) <= 2048 && M <= 256) return {0, 0, 0, 0, false};
   const int64_t tiles = (M + 31) / 32, blocks = (N + 63) / 64, jobs = (M + 63) / 64;
-  const bool order = M > 128 && M <= 1 << 17 && adapters >= 8 && adapters < 4096 && (int64_t)(scratch / 4) >= M * (R + 2);
+  const bool order = M > 128 && M <= 1 << 17 && M * std::min<int64_t>(adapters, 64) >= 8192 && adapters >= 8 && adapters < 4096 && (int64_t)(scratch / 4) >= M * (R + 2);
   // adapters of a tile: in order few, and two slots for tiles where one adapter's rows end and another's begin
   const int64_t kinds = order ? std::min<int64_t>(adapters, 1 + (adapters + jobs - 1) / jobs) : adapters;
   const int64_t room = order ? (int64_t)((scratch / 4 - 2 * M) / (M * R)) : fits;
