@@ -39,6 +39,8 @@ struct PtrFields<LoraArgs> {
 
 namespace {
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
 __device__ __forceinline__ uint4 zeros() { return make_uint4(0, 0, 0, 0); }
 __device__ __forceinline__ uint4 load16(const void* p) { return *reinterpret_cast<const uint4*>(p); }
 
@@ -57,7 +59,7 @@ __device__ __forceinline__ float rest_of(float t, uint16_t part) { return fabsf(
 
 // A lane's four outputs of a row: n, n + 1, .. where rows are vectors of four (vec), else n, n + 16, .. so that 16 lanes' are side by side.
 // The base's values there, loaded ahead (m: a row that is there; outputs behind N are not used).
-template <bool F32>
+template <bool F32, bool STREAM>
 struct Base {
   uint4 w;                // fp32, or bf16 pairs in x and y
   __device__ __forceinline__ void load(const Lora& a, bool vec, int64_t m, int n) {
@@ -67,7 +69,7 @@ struct Base {
     if constexpr (F32) {
       const uint32_t* p = static_cast<const uint32_t*>(a.base) + at;
       if (vec) {
-        w = load16(p);
+        w = STREAM ? load_nt16(p) : load16(p);
       } else {
         const int last = a.N - 1 - n;               // the last one again behind N
         w = make_uint4(p[0], p[min(16, last)], p[min(32, last)], p[min(48, last)]);
@@ -75,7 +77,10 @@ struct Base {
     } else {
       const uint16_t* p = static_cast<const uint16_t*>(a.base) + at;
       if (vec) {
-        const uint2 u = *reinterpret_cast<const uint2*>(p);
+        const u32x2* q = reinterpret_cast<const u32x2*>(p);
+        u32x2 u;
+        if constexpr (STREAM) u = __builtin_nontemporal_load(q);
+        else u = *q;
         w.x = u.x, w.y = u.y;
       } else {
         const int last = a.N - 1 - n;
@@ -102,12 +107,20 @@ __device__ __forceinline__ void activate(f32x4 (&v)[R], int act) {
 }
 
 // Row m's four outputs.
-template <bool F32>
+template <bool F32, bool STREAM>
 __device__ __forceinline__ void store(const Lora& a, bool vec, int64_t m, int n, f32x4 v) {
   const int64_t at = m * a.ldy + n;
   if (vec && n < a.N) {
-    if constexpr (F32) *reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at) = v;
-    else *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + at) = make_uint2(f2bf2(v[0], v[1]), f2bf2(v[2], v[3]));
+    if constexpr (F32) {
+      f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at);
+      if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+      else *p = v;
+    } else {
+      const u32x2 w = {f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+      u32x2* p = reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.y) + at);
+      if constexpr (STREAM) __builtin_nontemporal_store(w, p);
+      else *p = w;
+    }
     return;
   }
 #pragma unroll
@@ -221,16 +234,16 @@ __device__ __forceinline__ void lds_reads_done() { asm volatile("s_waitcnt lgkmc
 template <int N>
 __device__ __forceinline__ void vm_left() { asm volatile("s_waitcnt vmcnt(%0)" ::"i"(N) : "memory"); }
 
-// t[z][m][r] of the rows of 32 that name an adapter of this slot. The waves take steps of 64 k (a cache line of each row of x and A) in
+// t[z][m][r] of the rows of 16 T that name an adapter of this slot. The waves take steps of 64 k (a cache line of each row of x and A) in
 // turns, each through a ring of NST steps in LDS of its own, and join in wave order. The operands' lanes lie row by row, 16 bytes of
 // each: loaded so, a load takes 64 cycles of the address path (measured 15 bytes a cycle and CU, 42 us for 8192 rows of 4096, rank 64);
 // into LDS eight lanes bring a row's line. Its eight chunks are moved by key_of(row) so that 16 rows' same chunk falls on different banks.
 // RB: blocks of 16 ranks.
 __device__ __forceinline__ int key_of(int row) { return row >> 1 & 7; }
 
-template <int RB, int W, int NST>
+template <int T, int RB, int W, int NST>
 __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
-  constexpr int STAGE = 16 * (2 + RB) * 128, RING = NST * STAGE, JOIN = W * 16 * 33 * 4, LDS = W * RING > JOIN ? W * RING : JOIN;
+  constexpr int STAGE = 16 * (T + RB) * 128, RING = NST * STAGE, JOIN = W * 16 * (16 * T + 1) * 4, LDS = W * RING > JOIN ? W * RING : JOIN;
   static_assert(LDS <= 160 * 1024, "LDS");
   __shared__ __attribute__((aligned(1024))) char lds[LDS];
   const Lora& a = g.a;
@@ -240,8 +253,8 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
   const int z = at % g.splits;
   at /= g.splits;
   // slots last: the others' workgroups may have nothing to do
-  const int tiles = (a.M + 31) / 32, slot = at / tiles, m0 = tile_of(at % tiles, tiles) * 32;
-  const int2 place = place_of<32>(g, m0, lane);
+  const int tiles = (a.M + 16 * T - 1) / (16 * T), slot = at / tiles, m0 = tile_of(at % tiles, tiles) * 16 * T;
+  const int2 place = place_of<16 * T>(g, m0, lane);
   const int mine = place.y;
   const int full = a.K >> 6, stride = g.splits * W, s0 = z * W + wave, n = full > s0 ? (full - s0 + stride - 1) / stride : 0;
   const char* ring = lds + wave * RING;
@@ -319,7 +332,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
       }
     }
     const float scale = a.scales ? a.scales[ad] : 1.f;
-    float(*part)[16][33] = reinterpret_cast<float(*)[16][33]>(lds);
+    float(*part)[16][16 * T + 1] = reinterpret_cast<float(*)[16][16 * T + 1]>(lds);
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       __syncthreads();                              // (what was there has been read)
@@ -333,7 +346,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
         float t = 0.f;
 #pragma unroll
         for (int w = 0; w < W; ++w) t += part[w][i % 16][j];
-        const int row = __shfl(rows, min(j, 31), 64);
+        const int row = __shfl(rows, min(j, 63), 64);
         if (j < count && r < a.R) g.t[((int64_t)z * a.M + row) * a.R + r] = r < rank ? t * scale : 0.f;
       }
     }
@@ -346,7 +359,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
     left &= ~mask;
     if (j % g.slots != slot) continue;
     const int rows = __shfl(place.x, nth_of(mask, lane), 64), count = __builtin_popcountll(mask);
-    if (count > 16) body(std::integral_constant<int, 2>(), ad, rows, count);
+    if (count > 16) body(std::integral_constant<int, T>(), ad, rows, count);
     else body(std::integral_constant<int, 1>(), ad, rows, count);
   }
 }
@@ -357,7 +370,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
 // lanes of outputs are n = 64 nb + 4 l + e: a lane has four consecutive outputs of four rows, 16 lanes a row's 64 (16 e + l where rows
 // are no vectors of four). In LDS row 16 e + l holds that row of B, its chunks moved by at_of so that 16 rows' same chunk falls on
 // different banks.
-template <bool F32, int RC>
+template <bool F32, int RC, bool STREAM>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
   constexpr int W = 4, PARTS = F32 ? 3 : 2, ROWS = 16 * W, PITCH = 64 * RC, CPR = 4 * RC, MINE = CPR / W;
   __shared__ __attribute__((aligned(16))) char lds[2][64 * PITCH];
@@ -403,7 +416,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
         *reinterpret_cast<uint4*>(to + at_of(g.vec ? 16 * (row & 3) + (row >> 2) : row, ch)) = first_of(bw[i], rank - 8 * ch);
       }
     };
-    Base<F32> base[4];
+    Base<F32, STREAM> base[4];
     auto load_base = [&](int nb) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) base[i].load(a, g.vec, m[i], nb * 64 + lane_n);
@@ -479,7 +492,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
         activate(v, a.act);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (first + 4 * q4 + i < count) store<F32>(a, g.vec, m[i], nb * 64 + lane_n, v[i]);
+          if (first + 4 * q4 + i < count) store<F32, STREAM>(a, g.vec, m[i], nb * 64 + lane_n, v[i]);
       }
       if (rank && nb + 1 < nb1) {
         keep_b(lds[(nb + 1 - nb0) & 1], rank);
@@ -594,23 +607,23 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
   f32x4 v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    Base<F32> base;
+    Base<F32, false> base;
     base.load(a, g.vec, min(m0 + 4 * q4 + i, a.M - 1), n0 + (g.vec ? 4 * r16 : r16));
     v[i] = base.values() + f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
   }
   activate(v, a.act);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (m0 + 4 * q4 + i < a.M) store<F32>(a, g.vec, m0 + 4 * q4 + i, n0 + (g.vec ? 4 * r16 : r16), v[i]);
+    if (m0 + 4 * q4 + i < a.M) store<F32, false>(a, g.vec, m0 + 4 * q4 + i, n0 + (g.vec ? 4 * r16 : r16), v[i]);
 }
 
-template <bool F32>
+template <bool F32, bool STREAM>
 hipError_t up(LoraArgs g, hipStream_t s) {
   const int tiles = (g.a.M + 63) / 64;
   g.xcds = tiles < 8 ? 1 : 8;
   const unsigned wgs = (unsigned)((tiles + g.xcds - 1) / g.xcds * g.xcds) * g.slots * g.tiles_n;
   const int rc = (g.a.R + 31) / 32;
-  return launch(rc == 1 ? k_lora_up<F32, 1> : rc == 2 ? k_lora_up<F32, 2> : k_lora_up<F32, 4>, dim3(wgs), dim3(256), 0, s, g);
+  return launch(rc == 1 ? k_lora_up<F32, 1, STREAM> : rc == 2 ? k_lora_up<F32, 2, STREAM> : k_lora_up<F32, 4, STREAM>, dim3(wgs), dim3(256), 0, s, g);
 }
 
 }  // namespace
@@ -636,18 +649,21 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
     if (e != hipSuccess) return e;
   }
   g.slots = p.down_slots;
-  const unsigned tiles = (a.M + 31) / 32;
+  const unsigned tiles = p.tall ? (a.M + 63) / 64 : (a.M + 31) / 32;
   const int rb = (a.R + 15) / 16;
   const unsigned down = tiles * g.slots * g.splits;
-  const hipError_t e = rb == 1   ? launch(k_lora_down<1, 4, 2>, dim3(down), dim3(256), 0, s, g)
-                       : rb == 2 ? launch(k_lora_down<2, 4, 2>, dim3(down), dim3(256), 0, s, g)
-                       : rb <= 4 ? launch(k_lora_down<4, 3, 2>, dim3(down), dim3(192), 0, s, g)
-                                 : launch(k_lora_down<8, 4, 1>, dim3(down), dim3(256), 0, s, g);
+  const hipError_t e = rb == 1   ? launch(k_lora_down<2, 1, 4, 2>, dim3(down), dim3(256), 0, s, g)
+                       : rb == 2 ? launch(k_lora_down<2, 2, 4, 2>, dim3(down), dim3(256), 0, s, g)
+                       : p.tall  ? launch(k_lora_down<4, 4, 2, 2>, dim3(down), dim3(128), 0, s, g)
+                       : rb <= 4 ? launch(k_lora_down<2, 4, 3, 2>, dim3(down), dim3(192), 0, s, g)
+                                 : launch(k_lora_down<2, 8, 4, 1>, dim3(down), dim3(256), 0, s, g);
   if (e != hipSuccess) return e;
   g.slots = p.up_slots;
   g.run = p.run;
   g.tiles_n = (int)((((int64_t)a.N + 63) / 64 + g.run - 1) / g.run);
-  return a.f32 ? up<true>(g, s) : up<false>(g, s);
+  // A result of 16 MiB or more goes past the caches, as its base comes (8192 rows of 4096 x 4096, rank 64: 68 us instead of 77).
+  if ((int64_t)a.M * a.N * (a.f32 ? 4 : 2) >= 16 << 20) return a.f32 ? up<true, true>(g, s) : up<false, true>(g, s);
+  return a.f32 ? up<true, false>(g, s) : up<false, false>(g, s);
 }
 
 }  // namespace k

@@ -10,20 +10,23 @@ constexpr int kLoraRank = 128;          // the largest rank
 
 struct LoraPlan {
   int splits;             // workgroups along K; 0: both products in one launch, no scratch
-  int down_slots;         // workgroups that share the adapters of a tile of 32 rows, first product
-  int up_slots;           // and of 64 rows, second product
+  int tall;               // tiles of 64 rows, first product, else of 32
+  int down_slots;         // workgroups that share the adapters of such a tile
+  int up_slots;           // and of a tile of 64 rows, second product
   int run;                // blocks of 64 outputs a workgroup, second product
   bool order;             // rows adapter by adapter first
 };
 
 inline LoraPlan lora_plan(int64_t M, int64_t N, int64_t K, int64_t R, int64_t adapters, uint64_t scratch) {
   const int64_t fits = (int64_t)(scratch / 4) / (M * R);
-  if (fits < 1 || M >= 1 << 27) return {0, 0, 0, 0, false};
+  if (fits < 1 || M >= 1 << 27) return {0, 0, 0, 0, 0, false};
   // One adapter, small: in one launch (us, graph replay, one / two launches): 1 row of 768 x 768, rank 8 5.1 / 6.7, rank 64 9.0 / 8.7; 1 of
   // 4096 x 4096, rank 16 10.1 / 7.8; 256 of 256 x 256, rank 8 5.6 / 7.7. Adapters of one tile come one after the other
   // there: 64 rows of 8, 768 x 768, rank 8 26 / 8.5.
-  if (std::min(M, adapters) == 1 && K * ((R + 15) / 16) <= 2048 && M <= 256) return {0, 0, 0, 0, false};
-  const int64_t tiles = (M + 31) / 32, blocks = (N + 63) / 64, jobs = (M + 63) / 64;
+  if (std::min(M, adapters) == 1 && K * ((R + 15) / 16) <= 2048 && M <= 256) return {0, 0, 0, 0, 0, false};
+  // Tall tiles read A half as often, at ranks where that is most of what a CU reads: five adapters of 64, 8192 rows of 4096 20 us, else 25.
+  const bool tall = R > 32 && R <= 64 && M >= 4096 && K >= 1024;
+  const int64_t tiles = tall ? (M + 63) / 64 : (M + 31) / 32, blocks = (N + 63) / 64, jobs = (M + 63) / 64;
   const bool order = M > 128 && M <= 1 << 17 && M * std::min<int64_t>(adapters, 64) >= 8192 && adapters >= 8 && adapters < 4096 && (int64_t)(scratch / 4) >= M * (R + 2);
   // adapters of a tile: in order few, and two slots for tiles where one adapter's rows end and another's begin
   const int64_t kinds = order ? std::min<int64_t>(adapters, 1 + (adapters + jobs - 1) / jobs) : adapters;
@@ -32,7 +35,7 @@ inline LoraPlan lora_plan(int64_t M, int64_t N, int64_t K, int64_t R, int64_t ad
   const int64_t z = std::max<int64_t>(1, std::min<int64_t>({K / 512, 8, 512 / (tiles * ds), room}));
   const int64_t us = std::max<int64_t>(1, std::min<int64_t>({kinds, 64, M, std::max<int64_t>(2, 4096 / (jobs * blocks))}));
   const int64_t run = std::max<int64_t>(1, std::min<int64_t>(8, (jobs * blocks * us + 767) / 768));
-  return {(int)z, (int)ds, (int)us, (int)run, order};
+  return {(int)z, tall, (int)ds, (int)us, (int)run, order};
 }
 
 }  // namespace k

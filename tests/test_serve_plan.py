@@ -28,7 +28,7 @@ int main() {
     } else {                    // rows, outputs, inputs, rank, adapters, scratch
       if (std::scanf("%ld %ld %ld %ld %ld %lu", &a, &b, &c, &d, &e, &scratch) != 6) return 1;
       const LoraPlan p = lora_plan(a, b, c, d, e, scratch);
-      std::printf("%d %d %d %d %d\n", p.splits, p.down_slots, p.up_slots, p.run, (int)p.order);
+      std::printf("%d %d %d %d %d %d\n", p.splits, p.tall, p.down_slots, p.up_slots, p.run, (int)p.order);
     }
 }
 """
@@ -70,14 +70,14 @@ def test_the_gpu_shapes_reach_every_attention_kernel(plan, dim, e4m3):
 def test_the_gpu_shapes_reach_every_adapter_kernel(plan):
     calls = [(m, n, k, r, slots, SCRATCH) for _, m, k, n, r, slots, _ in LORA]
     reached = set()
-    for shape, (splits, _, _, run, order) in zip(LORA, plan("l", calls)):
+    for shape, (splits, tall, _, _, run, order) in zip(LORA, plan("l", calls)):
         r = shape[4]
         rb, rc = ((r + 15) // 16, (r + 31) // 32)
         rb, rc = (rb if rb < 3 else 4 if rb < 5 else 8), (rc if rc < 3 else 4)
         assert (rb, rc, splits, run > 1, bool(order)) == shape[0], (shape, splits, run, order)
-        reached |= {("down", rb), ("up", rc), ("order", bool(order)), ("run", run > 1)} if splits else {("one",)}
+        reached |= {("down", rb), ("tall", bool(tall)), ("up", rc), ("order", bool(order)), ("run", run > 1)} if splits else {("one",)}
     assert reached == {("one",), *(("down", i) for i in (1, 2, 4, 8)), *(("up", i) for i in (1, 2, 4)),
-                       *((w, b) for w in ("order", "run") for b in (False, True))}
+                       *((w, b) for w in ("tall", "order", "run") for b in (False, True))}
 
 
 def test_attention_plans_can_be_launched(plan):
@@ -109,12 +109,12 @@ def test_adapter_plans_can_be_launched(plan):
             continue                                             # refused before
         calls.append((m, n, 8 * rng.choice((1, 3, 2 ** rng.randint(0, 17))), 8 * rng.randint(1, 16), rng.choice((1, 2, 5, 8, 100, 5000, 10 ** 6)),
                       rng.choice((0, 4096, SCRATCH, 2 ** 40, 2 ** 63))))
-    for c, (splits, ds, us, run, order) in zip(calls, plan("l", calls)):
+    for c, (splits, tall, ds, us, run, order) in zip(calls, plan("l", calls)):
         m, n, _, r, adapters, scratch = c
         if splits == 0:
             continue                                             # (m + 15) / 16 times (n + 255) / 256 workgroups of 256
         assert splits >= 1 and ds >= 1 and us >= 1 and 1 <= run <= 8
-        assert (m + 31) // 32 * ds * splits * 256 < 2 ** 32, c
+        assert (m + 31) // 32 * ds * splits * 256 < 2 ** 32 and (not tall or 32 < r <= 64), c
         tiles = (m + 63) // 64
         assert (tiles if tiles < 8 else (tiles + 7) // 8 * 8) * us * -(-(-(-n // 64)) // run) * 256 < 2 ** 32, c
         assert 4 * m * (splits * r + (2 if order else 0)) <= scratch, c
