@@ -24,7 +24,6 @@ struct LoraArgs {
   int splits;             // over K
   int slots;              // workgroups (or waves) that share a tile's adapters
   int tiles_n;            // blocks of outputs
-  int vec;                // base and y four outputs at a time
   int run, xcds;          // second product: blocks of 64 outputs a workgroup, XCDs that tiles are handed to
 };
 
@@ -57,34 +56,41 @@ __device__ __forceinline__ int rank_of(const Lora& a, int ad) { return a.ranks ?
 // The rest of t behind its bf16 part (none behind an infinity or NaN).
 __device__ __forceinline__ float rest_of(float t, uint16_t part) { return fabsf(t) < INFINITY ? t - bf2f(part) : 0.f; }
 
-// A lane's four outputs of a row: n, n + 1, .. where rows are vectors of four (vec), else n, n + 16, .. so that 16 lanes' are side by side.
+// A lane's four consecutive outputs of a row as one vector, at any multiple of their element (one access on this hardware; as
+// single elements 3444 rows of 3592 x 5702, rank 128, took 119 us, so 87).
+typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+
 // The base's values there, loaded ahead (m: a row that is there; outputs behind N are not used).
 template <bool F32, bool STREAM>
 struct Base {
   uint4 w;                // fp32, or bf16 pairs in x and y
-  __device__ __forceinline__ void load(const Lora& a, bool vec, int64_t m, int n) {
+  __device__ __forceinline__ void load(const Lora& a, int64_t m, int n) {
     w = zeros();
     if (!a.base || n >= a.N) return;
     const int64_t at = m * a.ldbase + n;
+    const int last = a.N - 1 - n;                   // the last one again behind N
     if constexpr (F32) {
       const uint32_t* p = static_cast<const uint32_t*>(a.base) + at;
-      if (vec) {
-        w = STREAM ? load_nt16(p) : load16(p);
+      if (last >= 3) {
+        const u32x4_at4* q = reinterpret_cast<const u32x4_at4*>(p);
+        u32x4 u;
+        if constexpr (STREAM) u = __builtin_nontemporal_load(q);
+        else u = *q;
+        w = make_uint4(u.x, u.y, u.z, u.w);
       } else {
-        const int last = a.N - 1 - n;               // the last one again behind N
-        w = make_uint4(p[0], p[min(16, last)], p[min(32, last)], p[min(48, last)]);
+        w = make_uint4(p[0], p[min(1, last)], p[min(2, last)], 0);
       }
     } else {
       const uint16_t* p = static_cast<const uint16_t*>(a.base) + at;
-      if (vec) {
-        const u32x2* q = reinterpret_cast<const u32x2*>(p);
+      if (last >= 3) {
+        const u32x2_at2* q = reinterpret_cast<const u32x2_at2*>(p);
         u32x2 u;
         if constexpr (STREAM) u = __builtin_nontemporal_load(q);
         else u = *q;
         w.x = u.x, w.y = u.y;
       } else {
-        const int last = a.N - 1 - n;
-        w.x = p[0] | (uint32_t)p[min(16, last)] << 16, w.y = p[min(32, last)] | (uint32_t)p[min(48, last)] << 16;
+        w.x = p[0] | (uint32_t)p[min(1, last)] << 16, w.y = p[min(2, last)];
       }
     }
   }
@@ -108,26 +114,26 @@ __device__ __forceinline__ void activate(f32x4 (&v)[R], int act) {
 
 // Row m's four outputs.
 template <bool F32, bool STREAM>
-__device__ __forceinline__ void store(const Lora& a, bool vec, int64_t m, int n, f32x4 v) {
+__device__ __forceinline__ void store(const Lora& a, int64_t m, int n, f32x4 v) {
   const int64_t at = m * a.ldy + n;
-  if (vec && n < a.N) {
+  if (n <= a.N - 4) {
     if constexpr (F32) {
-      f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(a.y) + at);
-      if constexpr (STREAM) __builtin_nontemporal_store(v, p);
-      else *p = v;
+      u32x4_at4* p = reinterpret_cast<u32x4_at4*>(static_cast<float*>(a.y) + at);
+      if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(u32x4_at4, v), p);
+      else *p = __builtin_bit_cast(u32x4_at4, v);
     } else {
-      const u32x2 w = {f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
-      u32x2* p = reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.y) + at);
+      const u32x2_at2 w = {f2bf2(v[0], v[1]), f2bf2(v[2], v[3])};
+      u32x2_at2* p = reinterpret_cast<u32x2_at2*>(static_cast<uint16_t*>(a.y) + at);
       if constexpr (STREAM) __builtin_nontemporal_store(w, p);
       else *p = w;
     }
     return;
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (n + 16 * j >= a.N) continue;
-    if constexpr (F32) static_cast<float*>(a.y)[at + 16 * j] = v[j];
-    else static_cast<uint16_t*>(a.y)[at + 16 * j] = f2bf(v[j]);
+  for (int j = 0; j < 3; ++j) {
+    if (n + j >= a.N) continue;
+    if constexpr (F32) static_cast<float*>(a.y)[at + j] = v[j];
+    else static_cast<uint16_t*>(a.y)[at + j] = f2bf(v[j]);
   }
 }
 
@@ -367,8 +373,7 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
 // y of the rows of 64 that name an adapter of this slot (and in slot 0 those without one), g.run blocks of 64 outputs. The rows of one
 // adapter go to the waves, 16 to each; the parts of t stay in registers. A block of B (64 rows, in memory as they lie) goes through
 // registers into LDS, two blocks in turn, so that the next one's values and base are under way while one is computed. Product e's 16
-// lanes of outputs are n = 64 nb + 4 l + e: a lane has four consecutive outputs of four rows, 16 lanes a row's 64 (16 e + l where rows
-// are no vectors of four). In LDS row 16 e + l holds that row of B, its chunks moved by at_of so that 16 rows' same chunk falls on
+// lanes of outputs are n = 64 nb + 4 l + e: a lane has four consecutive outputs of four rows, 16 lanes a row's 64. In LDS row 16 e + l holds that row of B, its chunks moved by at_of so that 16 rows' same chunk falls on
 // different banks.
 template <bool F32, int RC, bool STREAM>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
@@ -385,7 +390,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
   const int m0 = tile * ROWS, nb0 = part * g.run, nb1 = min(nb0 + g.run, (a.N + 63) / 64);
   auto at_of = [](int row, int ch) { return row * PITCH + ((ch ^ (RC == 1 ? row >> 2 & 3 : RC == 2 ? row >> 1 & 7 : row & 15)) << 4); };
   const int2 place = place_of<ROWS>(g, m0, lane);
-  const int mine = place.y, lane_n = g.vec ? 4 * r16 : r16;
+  const int mine = place.y, lane_n = 4 * r16;
 
   // the rows whose bits are set in `mask`: of adapter ad (-1: none), or of none
   auto body = [&](int ad, unsigned long long mask) __attribute__((always_inline)) {
@@ -413,13 +418,13 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
 #pragma unroll
       for (int i = 0; i < MINE; ++i) {
         const int at = i * 64 * W + tid, row = at / CPR, ch = at % CPR;
-        *reinterpret_cast<uint4*>(to + at_of(g.vec ? 16 * (row & 3) + (row >> 2) : row, ch)) = first_of(bw[i], rank - 8 * ch);
+        *reinterpret_cast<uint4*>(to + at_of(16 * (row & 3) + (row >> 2), ch)) = first_of(bw[i], rank - 8 * ch);
       }
     };
     Base<F32, STREAM> base[4];
     auto load_base = [&](int nb) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) base[i].load(a, g.vec, m[i], nb * 64 + lane_n);
+      for (int i = 0; i < 4; ++i) base[i].load(a, m[i], nb * 64 + lane_n);
     };
     // everything that is read goes under way before anything is waited for, the rank among it
     if (ad >= 0) load_b(nb0);
@@ -492,7 +497,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
         activate(v, a.act);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (first + 4 * q4 + i < count) store<F32, STREAM>(a, g.vec, m[i], nb * 64 + lane_n, v[i]);
+          if (first + 4 * q4 + i < count) store<F32, STREAM>(a, m[i], nb * 64 + lane_n, v[i]);
       }
       if (rank && nb + 1 < nb1) {
         keep_b(lds[(nb + 1 - nb0) & 1], rank);
@@ -590,7 +595,7 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
       for (int p = 0; p < PARTS; ++p) tf[p] = as_bf16x8(load16(&ts[p][r16][r]));
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int n = n0 + (g.vec ? 4 * r16 + e : 16 * e + r16);
+        const int n = n0 + 4 * r16 + e;
         const uint4 bf = n < a.N && r < rank ? first_of(load16(up + (int64_t)n * a.R + r), rank - r) : zeros();
 #pragma unroll
         for (int p = 0; p < PARTS; ++p) y[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tf[p], as_bf16x8(bf), y[e], 0, 0, 0);
@@ -608,13 +613,13 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     Base<F32, false> base;
-    base.load(a, g.vec, min(m0 + 4 * q4 + i, a.M - 1), n0 + (g.vec ? 4 * r16 : r16));
+    base.load(a, min(m0 + 4 * q4 + i, a.M - 1), n0 + 4 * r16);
     v[i] = base.values() + f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
   }
   activate(v, a.act);
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (m0 + 4 * q4 + i < a.M) store<F32, false>(a, g.vec, m0 + 4 * q4 + i, n0 + (g.vec ? 4 * r16 : r16), v[i]);
+    if (m0 + 4 * q4 + i < a.M) store<F32, false>(a, m0 + 4 * q4 + i, n0 + 4 * r16, v[i]);
 }
 
 template <bool F32, bool STREAM>
@@ -636,8 +641,6 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   g.a = a;
   g.t = sp.partials;
   g.tiles_n = (int)(((int64_t)a.N + 255) / 256);
-  const uintptr_t four = a.f32 ? 16 : 8;
-  g.vec = a.N % 4 == 0 && (uintptr_t)a.y % four == 0 && a.ldy % 4 == 0 && (uintptr_t)a.base % four == 0 && a.ldbase % 4 == 0;
   if (((int64_t)a.M + 15) / 16 * g.tiles_n >= 1 << 24) return hipErrorInvalidValue;
   const LoraPlan p = lora_plan(a.M, a.N, a.K, a.R, a.adapters, sp.partials ? sp.partial_bytes : 0);
   if (p.splits == 0)
@@ -661,8 +664,11 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   g.slots = p.up_slots;
   g.run = p.run;
   g.tiles_n = (int)((((int64_t)a.N + 63) / 64 + g.run - 1) / g.run);
-  // A result of 16 MiB or more goes past the caches, as its base comes (8192 rows of 4096 x 4096, rank 64: 68 us instead of 77).
-  if ((int64_t)a.M * a.N * (a.f32 ? 4 : 2) >= 16 << 20) return a.f32 ? up<true, true>(g, s) : up<false, true>(g, s);
+  // A result of 16 MiB or more goes past the caches, as its base comes, where rows are whole lines of 128 bytes (8192 rows of 4096 x
+  // 4096, rank 64: 69 us instead of 78; 8191 rows of 4096 x 4099, whose lines are written in two parts, 104 so and 85 through the caches).
+  const int64_t item = a.f32 ? 4 : 2;
+  const bool lines = (((uintptr_t)a.y | (uintptr_t)a.base | (uintptr_t)(a.ldy * item) | (uintptr_t)(a.ldbase * item)) & 127) == 0;
+  if (lines && (int64_t)a.M * a.N * item >= 16 << 20) return a.f32 ? up<true, true>(g, s) : up<false, true>(g, s);
   return a.f32 ? up<true, false>(g, s) : up<false, false>(g, s);
 }
 

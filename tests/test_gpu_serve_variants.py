@@ -40,7 +40,8 @@ LORA = [
     ((2, 1, 1, True, False), 90, 64, 26000, 32, 5, grouped),
     ((4, 2, 2, False, False), 33, 1104, 70, 56, 4, mixed),
     ((4, 2, 1, False, True), 450, 520, 270, 40, 20, mixed),
-    ((4, 2, 2, True, False), 4100, 1032, 2052, 56, 3, grouped),
+    ((4, 2, 2, True, False), 4100, 1032, 2112, 56, 3, grouped),      # results past the caches
+    ((1, 1, 1, True, False), 4200, 520, 2051, 16, 1, grouped),       # as many, whose rows are no whole lines
     ((8, 4, 1, True, True), 920, 200, 3300, 104, 9, mixed),
     ((8, 4, 2, False, False), 40, 1032, 66, 128, 2, grouped),
     ((1, 1, 8, False, False), 2, 4104, 64, 8, 2, mixed),
