@@ -5,7 +5,8 @@
 // rows, finds the adapters that they name (the rows' numbers lie one in a lane; a ballot gives an adapter's rows), and takes
 // the rows of one adapter together, in blocks of 16, wherever in the tile they stand: rows of many requests in any order need no
 // sorting, and no row meets another's adapter. Where there are few tiles, the adapters of a tile go to several workgroups.
-// Where many tiles could hold many adapters each, k_lora_order first writes down the rows adapter by adapter, and tiles are of that order.
+// Where many tiles could hold many adapters each, k_lora_order first writes down the rows adapter by adapter, and tiles are of that order;
+// where a tile holds few, one more workgroup of k_lora_down does so for k_lora_up.
 // Without scratch k_lora does both in one launch and computes t anew for every 256 outputs.
 //
 // t is taken as bf16 parts (two, three for fp32 results: 2^-16 and 2^-24 of t), all multiplied by B, whose values are bf16 as they are.
@@ -21,6 +22,7 @@ struct LoraArgs {
   Lora a;
   float* t;               // [splits][M][R]
   int2* order;            // [M] rows and their adapters (-1: none), adapter by adapter; NULL: as they stand
+  int2* order_out;        // what one more workgroup of the first product writes for the second, or NULL
   int splits;             // over K
   int slots;              // workgroups (or waves) that share a tile's adapters
   int tiles_n;            // blocks of outputs
@@ -33,6 +35,7 @@ struct PtrFields<LoraArgs> {
     PtrFields<Lora>::add(v, at + (uint32_t)offsetof(LoraArgs, a));
     v.push_back(at + (uint32_t)offsetof(LoraArgs, t));
     v.push_back(at + (uint32_t)offsetof(LoraArgs, order));
+    v.push_back(at + (uint32_t)offsetof(LoraArgs, order_out));
   }
 };
 
@@ -232,6 +235,70 @@ __device__ __forceinline__ int tile_of(int id, int tiles) {
   return id >= each * 8 + more ? id : x * each + min(x, more) + (id >> 3);
 }
 
+// The same order for up to seven adapters and kLoraFewRows rows, by one workgroup of W waves: every lane has a run of rows, whose
+// bins (the adapter, or none) lie in LDS a byte each; it counts them in eight packed counters, the counts are summed up over the lanes
+// before, and it puts its rows in their places. Every adapter's rows keep their order.
+template <int W>
+__device__ __forceinline__ void order_few(const Lora& a, int2* order, char* lds, int wave, int lane) {
+  constexpr int T = 64 * W, AHEAD = 8, kSums = 20 * 1024;
+  static_assert(kLoraFew < 8 && kLoraFewRows + 4 * 2 * T <= kSums && kLoraFewRows < 1 << 15, "packed counters");
+  const int tid = wave * 64 + lane, none = a.adapters, words = ((a.M + 4 * T - 1) / (4 * T)) | 1;      // of a lane; odd: no bank conflicts
+  for (int m0 = tid; m0 - tid < words * 4 * T; m0 += T * AHEAD) {
+    int id[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) id[i] = a.adapter[min(m0 + i * T, a.M - 1)];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int m = m0 + i * T;
+      if (m < words * 4 * T) lds[m] = m >= a.M ? 8 : (unsigned)id[i] < (unsigned)none ? (char)id[i] : (char)none;
+    }
+  }
+  __syncthreads();
+  const uint32_t* mine = reinterpret_cast<const uint32_t*>(lds) + tid * words;
+  // 16 bits a bin, four to a word
+  uint64_t lo = 0, hi = 0;
+  for (int i = 0; i < words; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t bin = mine[i] >> (8 * e) & 255u;
+      const uint64_t one = 1ull << (16 * (bin & 3));
+      lo += bin < 4 ? one : 0;
+      hi += bin >= 4 && bin < 8 ? one : 0;
+    }
+  uint64_t lo_to = lo, hi_to = hi;                  // of the lanes up to this one
+#pragma unroll
+  for (int step = 1; step < 64; step *= 2) {
+    const uint64_t l = __shfl_up(lo_to, step, 64), h = __shfl_up(hi_to, step, 64);
+    if (lane >= step) lo_to += l, hi_to += h;
+  }
+  uint64_t* sums = reinterpret_cast<uint64_t*>(lds + kSums);
+  if (lane == 63) sums[2 * wave] = lo_to, sums[2 * wave + 1] = hi_to;
+  __syncthreads();
+  uint64_t lo_all = 0, hi_all = 0;
+  lo_to -= lo, hi_to -= hi;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    lo_all += sums[2 * w], hi_all += sums[2 * w + 1];
+    if (w < wave) lo_to += sums[2 * w], hi_to += sums[2 * w + 1];
+  }
+  // the bins before: x times 1 + 2^16 + 2^32 + 2^48 sums up the four counts in front of and in each
+  lo_all *= 0x0001000100010001ull;
+  hi_all *= 0x0001000100010001ull;
+  lo_to += lo_all << 16;
+  hi_to += (hi_all << 16) + (lo_all >> 48) * 0x0001000100010001ull;
+  const int m0 = tid * words * 4;
+  for (int i = 0; i < words; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t bin = mine[i] >> (8 * e) & 255u;
+      const int at = (int)((bin < 4 ? lo_to : hi_to) >> (16 * (bin & 3)) & 0xffffu);
+      const uint64_t one = 1ull << (16 * (bin & 3));
+      lo_to += bin < 4 ? one : 0;
+      hi_to += bin >= 4 && bin < 8 ? one : 0;
+      if (bin < 8) order[at] = make_int2(m0 + 4 * i + e, (int)bin < none ? (int)bin : -1);
+    }
+}
+
 // 16 bytes per lane straight into LDS: lane l's land at `dst` + 16 l. (m0 is set in the block, which holds the wait state behind it.)
 __device__ __forceinline__ void lane_to_lds(const void* p, uint32_t dst) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(dst), "v"(p) : "m0");
@@ -250,12 +317,16 @@ __device__ __forceinline__ int key_of(int row) { return row >> 1 & 7; }
 template <int T, int RB, int W, int NST>
 __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
   constexpr int STAGE = 16 * (T + RB) * 128, RING = NST * STAGE, JOIN = W * 16 * (16 * T + 1) * 4, LDS = W * RING > JOIN ? W * RING : JOIN;
-  static_assert(LDS <= 160 * 1024, "LDS");
+  static_assert(LDS <= 160 * 1024 && LDS >= 21 * 1024, "LDS");
   __shared__ __attribute__((aligned(1024))) char lds[LDS];
   const Lora& a = g.a;
   const int tid = threadIdx.x, lane = tid & 63, r16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int at = blockIdx.x;
+  if (g.order_out) {                                // the first of the workgroups
+    if (at == 0) return order_few<W>(a, g.order_out, lds, wave, lane);
+    --at;
+  }
   const int z = at % g.splits;
   at /= g.splits;
   // slots last: the others' workgroups may have nothing to do
@@ -646,21 +717,24 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   if (p.splits == 0)
     return launch(a.f32 ? k_lora<true> : k_lora<false>, dim3((unsigned)((a.M + 15) / 16 * g.tiles_n)), dim3(64 * kWaves), 0, s, g);
   g.splits = p.splits;
-  if (p.order) {
-    g.order = reinterpret_cast<int2*>(g.t + (int64_t)p.splits * a.M * a.R);       // (R is even: at 8 bytes)
+  int2* const order = reinterpret_cast<int2*>(g.t + (int64_t)p.splits * a.M * a.R);       // (R is even: at 8 bytes)
+  if (p.order == 1) {
+    g.order = order;
     const hipError_t e = launch(k_lora_order, dim3(1), dim3(1024), 0, s, g);
     if (e != hipSuccess) return e;
   }
+  g.order_out = p.order == 2 ? order : nullptr;
   g.slots = p.down_slots;
   const unsigned tiles = p.tall ? (a.M + 63) / 64 : (a.M + 31) / 32;
   const int rb = (a.R + 15) / 16;
-  const unsigned down = tiles * g.slots * g.splits;
+  const unsigned down = tiles * g.slots * g.splits + (p.order == 2);
   const hipError_t e = rb == 1   ? launch(k_lora_down<2, 1, 4, 2>, dim3(down), dim3(256), 0, s, g)
                        : rb == 2 ? launch(k_lora_down<2, 2, 4, 2>, dim3(down), dim3(256), 0, s, g)
                        : p.tall  ? launch(k_lora_down<4, 4, 2, 2>, dim3(down), dim3(128), 0, s, g)
                        : rb <= 4 ? launch(k_lora_down<2, 4, 3, 2>, dim3(down), dim3(192), 0, s, g)
                                  : launch(k_lora_down<2, 8, 4, 1>, dim3(down), dim3(256), 0, s, g);
   if (e != hipSuccess) return e;
+  if (p.order) g.order = order;
   g.slots = p.up_slots;
   g.run = p.run;
   g.tiles_n = (int)((((int64_t)a.N + 63) / 64 + g.run - 1) / g.run);

@@ -30,21 +30,25 @@ ATTENTION = [
     ((4, 4, True), 33, 4, 2, 64, [4000], {"sinks": 5, "window": 3000}),
 ]
 
-# (ranks' blocks of 16 and chunks of 32, splits of K or 0 for one launch, several runs, in order first), rows, inputs, outputs, rank,
+# (ranks' blocks of 16 and chunks of 32, splits of K or 0 for one launch, several runs, in order first (1) or beside (2)), rows, inputs, outputs, rank,
 # adapters, rows' adapters
 LORA = [
-    ((1, 1, 0, False, False), 1, 704, 300, 16, 3, mixed),
-    ((1, 1, 0, False, False), 200, 248, 130, 8, 1, grouped),
-    ((1, 1, 4, False, False), 5, 2048, 200, 16, 3, mixed),
-    ((2, 1, 1, False, False), 60, 104, 90, 24, 9, mixed),
-    ((2, 1, 1, True, False), 90, 64, 26000, 32, 5, grouped),
-    ((4, 2, 2, False, False), 33, 1104, 70, 56, 4, mixed),
-    ((4, 2, 1, False, True), 450, 520, 270, 40, 20, mixed),
-    ((4, 2, 2, True, False), 4100, 1032, 2112, 56, 3, grouped),      # results past the caches
-    ((1, 1, 1, True, False), 4200, 520, 2051, 16, 1, grouped),       # as many, whose rows are no whole lines
-    ((8, 4, 1, True, True), 920, 200, 3300, 104, 9, mixed),
-    ((8, 4, 2, False, False), 40, 1032, 66, 128, 2, grouped),
-    ((1, 1, 8, False, False), 2, 4104, 64, 8, 2, mixed),
+    ((1, 1, 0, False, 0), 1, 704, 300, 16, 3, mixed),
+    ((1, 1, 0, False, 0), 200, 248, 130, 8, 1, grouped),
+    ((1, 1, 4, False, 0), 5, 2048, 200, 16, 3, mixed),
+    ((2, 1, 1, False, 0), 60, 104, 90, 24, 9, mixed),
+    ((2, 1, 1, True, 0), 90, 64, 26000, 32, 5, grouped),
+    ((4, 2, 2, False, 0), 33, 1104, 70, 56, 4, mixed),
+    ((4, 2, 1, False, 1), 450, 520, 270, 40, 20, mixed),
+    ((4, 2, 2, True, 2), 4100, 1032, 2112, 56, 3, grouped),      # results past the caches
+    ((1, 1, 1, True, 0), 4200, 520, 2051, 16, 1, grouped),       # as many, whose rows are no whole lines
+    ((8, 4, 1, True, 1), 920, 200, 3300, 104, 9, mixed),
+    ((8, 4, 2, False, 0), 40, 1032, 66, 128, 2, grouped),
+    ((1, 1, 1, False, 2), 777, 520, 131, 16, 7, mixed),
+    ((2, 1, 1, False, 2), 1025, 512, 64, 32, 2, mixed),
+    ((4, 2, 2, True, 2), 600, 1024, 3000, 64, 3, mixed),
+    ((8, 4, 1, False, 2), 8191, 520, 70, 72, 5, mixed),
+    ((1, 1, 8, False, 0), 2, 4104, 64, 8, 2, mixed),
 ]
 
 
