@@ -446,8 +446,13 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
 // registers into LDS, two blocks in turn, so that the next one's values and base are under way while one is computed. Product e's 16
 // lanes of outputs are n = 64 nb + 4 l + e: a lane has four consecutive outputs of four rows, 16 lanes a row's 64. In LDS row 16 e + l holds that row of B, its chunks moved by at_of so that 16 rows' same chunk falls on
 // different banks.
-template <bool F32, int RC, bool STREAM>
+// HOW: kPast: results go past the caches; kParts: t is in several parts (few rows; without the code for that, results of many rows have
+// a third wave on each SIMD: 8192 rows of 4096 x 4096, rank 64 70 us instead of 80).
+enum { kWhole, kPast, kParts };
+
+template <bool F32, int RC, int HOW>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
+  constexpr bool STREAM = HOW == kPast;
   constexpr int W = 4, PARTS = F32 ? 3 : 2, ROWS = 16 * W, PITCH = 64 * RC, CPR = 4 * RC, MINE = CPR / W;
   __shared__ __attribute__((aligned(16))) char lds[2][64 * PITCH];
   const Lora& a = g.a;
@@ -513,11 +518,30 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
     const int rank = ad < 0 ? 0 : rank_of(a, ad);
     uint4 tf[RC][PARTS];
     if (rank && busy) {
-      for (int z = 1; z < g.splits; ++z)
+      // the parts in their order, a few asked for at once (one behind the other, 64 rows of 24 adapters, 4096 x 4096, rank 16 / 128 took
+      // 11.7 / 24.8 us, so 10.7 / 18.0)
+      if constexpr (HOW == kParts) {
+        auto add = [&](auto count, int z0) __attribute__((always_inline)) {
+          constexpr int Z = decltype(count)::value;
+          f32x4 more[Z][RC][2];
 #pragma unroll
-        for (int rc = 0; rc < RC; ++rc)
+          for (int u = 0; u < Z; ++u)
 #pragma unroll
-          for (int i = 0; i < 2; ++i) tv[rc][i] += load_t(z, rc, i);
+            for (int rc = 0; rc < RC; ++rc)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) more[u][rc][i] = load_t(z0 + u, rc, i);
+#pragma unroll
+          for (int u = 0; u < Z; ++u)
+#pragma unroll
+            for (int rc = 0; rc < RC; ++rc)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) tv[rc][i] += more[u][rc][i];
+        };
+        constexpr int Z = RC == 1 ? 7 : RC == 2 ? 3 : 2;
+        int z = 1;
+        for (; z + Z <= g.splits; z += Z) add(std::integral_constant<int, Z>(), z);
+        for (; z < g.splits; ++z) add(std::integral_constant<int, 1>(), z);
+      }
 #pragma unroll
       for (int rc = 0; rc < RC; ++rc) {
         const int held = has ? rank - rc * 32 - 8 * q4 : 0;                             // of this lane's eight ranks
@@ -693,13 +717,13 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
     if (m0 + 4 * q4 + i < a.M) store<F32, false>(a, m0 + 4 * q4 + i, n0 + 4 * r16, v[i]);
 }
 
-template <bool F32, bool STREAM>
+template <bool F32, int HOW>
 hipError_t up(LoraArgs g, hipStream_t s) {
   const int tiles = (g.a.M + 63) / 64;
   g.xcds = tiles < 8 ? 1 : 8;
   const unsigned wgs = (unsigned)((tiles + g.xcds - 1) / g.xcds * g.xcds) * g.slots * g.tiles_n;
   const int rc = (g.a.R + 31) / 32;
-  return launch(rc == 1 ? k_lora_up<F32, 1, STREAM> : rc == 2 ? k_lora_up<F32, 2, STREAM> : k_lora_up<F32, 4, STREAM>, dim3(wgs), dim3(256), 0, s, g);
+  return launch(rc == 1 ? k_lora_up<F32, 1, HOW> : rc == 2 ? k_lora_up<F32, 2, HOW> : k_lora_up<F32, 4, HOW>, dim3(wgs), dim3(256), 0, s, g);
 }
 
 }  // namespace
@@ -742,8 +766,9 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   // 4096, rank 64: 69 us instead of 78; 8191 rows of 4096 x 4099, whose lines are written in two parts, 104 so and 85 through the caches).
   const int64_t item = a.f32 ? 4 : 2;
   const bool lines = (((uintptr_t)a.y | (uintptr_t)a.base | (uintptr_t)(a.ldy * item) | (uintptr_t)(a.ldbase * item)) & 127) == 0;
-  if (lines && (int64_t)a.M * a.N * item >= 16 << 20) return a.f32 ? up<true, true>(g, s) : up<false, true>(g, s);
-  return a.f32 ? up<true, false>(g, s) : up<false, false>(g, s);
+  if (g.splits > 1) return a.f32 ? up<true, kParts>(g, s) : up<false, kParts>(g, s);
+  if (lines && (int64_t)a.M * a.N * item >= 16 << 20) return a.f32 ? up<true, kPast>(g, s) : up<false, kPast>(g, s);
+  return a.f32 ? up<true, kWhole>(g, s) : up<false, kWhole>(g, s);
 }
 
 }  // namespace k

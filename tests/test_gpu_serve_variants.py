@@ -40,7 +40,10 @@ LORA = [
     ((2, 1, 1, True, 0), 90, 64, 26000, 32, 5, grouped),
     ((4, 2, 2, False, 0), 33, 1104, 70, 56, 4, mixed),
     ((4, 2, 1, False, 1), 450, 520, 270, 40, 20, mixed),
-    ((4, 2, 2, True, 2), 4100, 1032, 2112, 56, 3, grouped),      # results past the caches
+    ((4, 2, 2, True, 2), 4100, 1032, 2112, 56, 3, grouped),
+    ((1, 1, 1, True, 0), 4200, 520, 2112, 16, 1, grouped),       # results past the caches
+    ((4, 2, 1, True, 0), 4200, 200, 2112, 64, 1, grouped),
+    ((8, 4, 1, True, 0), 4200, 200, 2112, 128, 1, grouped),
     ((1, 1, 1, True, 0), 4200, 520, 2051, 16, 1, grouped),       # as many, whose rows are no whole lines
     ((8, 4, 1, True, 1), 920, 200, 3300, 104, 9, mixed),
     ((8, 4, 2, False, 0), 40, 1032, 66, 128, 2, grouped),
