@@ -208,3 +208,34 @@ def test_streams_and_captured_graphs():
                 g.replay()
         torch.cuda.synchronize()
         assert all(bool((o == w).all()) for (_, o), w in zip(calls, want)), turn
+
+
+@pytest.mark.parametrize("m,k,n,r,slots", [(1100, 640, 203, 40, 5), (513, 512, 65, 8, 7), (4096, 1024, 70, 64, 2), (600, 520, 131, 24, 19)])
+def test_rows_put_in_order(m, k, n, r, slots):
+    """Rows that come in order, in turn and at random, few or all of them without an adapter, in place, captured once for all of them."""
+    import paper_2306_03622_amd as tp
+    import torch
+    rng = np.random.default_rng(m)
+    orders = [grouped(m, slots), mixed(m, slots), rng.integers(-2, slots + 3, m).tolist(), [slots - 1] * m, [-1] * (m - 1) + [0], [slots] * m]
+    s = Setup(9, m, k, n, r, slots, False, orders[0], [max(1, r - 5 * a) for a in range(slots)])
+    out, work = s.base.clone(), scratch()
+
+    def call():
+        out.copy_(s.base)
+        tp.tps_lora(s.x, s.a, s.b, s.adapter, out, base=out, ranks=s.ranks, scales=s.scales, act="relu", work=work)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for turn, ids in enumerate(orders + orders[:2]):
+        s.adapter.copy_(torch.tensor(ids, dtype=torch.int32))
+        want = s.run("relu")
+        log(f"order {turn}")
+        s.check(want, "relu")
+        out.fill_(-3)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert bool((out == want).all()), turn

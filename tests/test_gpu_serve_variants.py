@@ -51,6 +51,8 @@ LORA = [
     ((2, 1, 1, False, 2), 1025, 512, 64, 32, 2, mixed),
     ((4, 2, 2, True, 2), 600, 1024, 3000, 64, 3, mixed),
     ((8, 4, 1, False, 2), 8191, 520, 70, 72, 5, mixed),
+    ((1, 1, 1, False, 2), 16384, 1024, 64, 8, 7, mixed),             # the most rows beside the first product
+    ((4, 2, 1, True, 2), 16383, 1032, 70, 40, 2, grouped),
     ((1, 1, 8, False, 0), 2, 4104, 64, 8, 2, mixed),
 ]
 
