@@ -467,14 +467,17 @@ __global__ __launch_bounds__(64 * W) void k_cache_attention(CacheAttnArgs g) {
   }
 }
 
-// Joins the splits of a row in split order: a wave per row. All that it reads, the first 16 splits' sums among it, is asked for at
-// once; what belongs to a row that has no query is read and dropped (one read behind the other took 4.7 us for two splits).
-template <int D>
+// Joins the splits of a row in split order: a wave per row, or WIDE a workgroup, whose waves take 16 splits each. All that it reads, the
+// first 16 splits' sums among it, is asked for at once; what belongs to a row that has no query is read and dropped (one read behind
+// the other took 4.7 us for two splits).
+template <int D, bool WIDE>
 __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs g) {
   constexpr int E = D / 64, Z = 16;
+  __shared__ float sums[WIDE ? 3 : 1][E][64];
   const CacheAttention& a = g.a;
   const int lane = threadIdx.x & 63;
-  const int64_t slot = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), first = WIDE ? wave * Z : 0;
+  const int64_t slot = WIDE ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   const int all = a.p.q_len * g.share;
   const int64_t slots = (int64_t)a.p.batch * a.c.heads * all;
   if (slot >= slots) return;
@@ -493,22 +496,33 @@ __global__ __launch_bounds__(256) void k_cache_join(CacheAttnArgs g) {
 #pragma unroll
       for (int e = 0; e < E; ++e) p[i][e] = z0 + i < g.splits ? g.part[((z0 + i) * slots + slot) * D + lane * E + e] : 0.f;
   };
-  load(0);
-  if (qi >= live) return;
+  load(first);
+  if (qi >= live) return;                           // (WIDE: the whole workgroup)
   float top = v.x;
 #pragma unroll
   for (int m = 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
   const float f = __builtin_amdgcn_exp2f(v.x - (top == -INFINITY ? 0.f : top));
   const float total = wave_sum(f * v.y);
   float o[E] = {};
-  for (int z0 = 0; z0 < g.splits; z0 += Z) {
-    if (z0) load(z0);
+  for (int z0 = first; z0 < (WIDE ? first + 1 : g.splits); z0 += Z) {
+    if (!WIDE && z0) load(z0);
 #pragma unroll
     for (int i = 0; i < Z; ++i) {
       const float fz = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), min(z0 + i, 63)));
 #pragma unroll
       for (int e = 0; e < E; ++e) o[e] += z0 + i < g.splits ? fz * p[i][e] : 0.f;
     }
+  }
+  if constexpr (WIDE) {
+    if (wave > 0)
+#pragma unroll
+      for (int e = 0; e < E; ++e) sums[wave - 1][e][lane] = o[e];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int w = 0; w < 3; ++w)
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += sums[w][e][lane];
   }
   const float inv = 1.f / total;
 #pragma unroll
@@ -526,7 +540,10 @@ hipError_t go(CacheAttnArgs g, hipStream_t s) {
   if (wgs * 64 * W >= 1ll << 32) return hipErrorInvalidValue;
   hipError_t e = launch((k_cache_attention<D, E4M3, RB, W, NST>), dim3((unsigned)wgs), dim3(64 * W), 0, s, g);
   if (e != hipSuccess || g.splits == 1) return e;
-  return launch((k_cache_join<D>), dim3((unsigned)((rows * heads + 3) / 4)), dim3(256), 0, s, g);
+  // A workgroup per row where its splits are more than a wave asks for at once, and rows few (us, a wave / a workgroup: one token of 8 heads
+  // on one, 64 values, over 60,000 21.6 / 15.5; two of 4096 11.0 / 9.4; one of 32 heads over 100,001 in 8 bits 49.7 / 48.7).
+  if (g.splits > 16 && rows * heads <= 4096) return launch((k_cache_join<D, true>), dim3((unsigned)(rows * heads)), dim3(256), 0, s, g);
+  return launch((k_cache_join<D, false>), dim3((unsigned)((rows * heads + 3) / 4)), dim3(256), 0, s, g);
 }
 
 template <int D, bool E4M3>
