@@ -79,7 +79,7 @@ TP_API tp_status tps_cache_read(const tps_cache_rows_args* a, void* stream);
  * most. Values of which 2^8 times a query's sum reaches 2^128 may overflow. An infinity or NaN in a seen v_j makes its
  * column infinite or NaN.
  * q and out: bf16, `heads` heads (each key/value head serves heads / kv_heads consecutive ones), strides in elements between
- * sequences, tokens and heads, as in tpo_attention (out's not 0). Made for single tokens and a few drafted ones: keys are
+ * sequences, tokens and heads, as in tpo_attention (out's not 0; it overlaps no input). Made for single tokens and a few drafted ones: keys are
  * read once for every 64 rows of q_len heads / kv_heads. batch * q_len * heads is below 2^27, batch * kv_heads below 2^22.
  * q_len or batch 0 does nothing. */
 typedef struct {
