@@ -447,8 +447,10 @@ __global__ __launch_bounds__(64 * W) void k_lora_down(LoraArgs g) {
 // lanes of outputs are n = 64 nb + 4 l + e: a lane has four consecutive outputs of four rows, 16 lanes a row's 64. In LDS row 16 e + l holds that row of B, its chunks moved by at_of so that 16 rows' same chunk falls on
 // different banks.
 // HOW: kPast: results go past the caches; kParts: t is in several parts (few rows; without the code for that, results of many rows have
-// a third wave on each SIMD: 8192 rows of 4096 x 4096, rank 64 70 us instead of 80).
-enum { kWhole, kPast, kParts };
+// a third wave on each SIMD: 8192 rows of 4096 x 4096, rank 64 70 us instead of 80). kFew, kFewParts: adapters of few rows are
+// likely, the rank is 32 at most; they take up to 16 rows of an adapter without LDS, a block of outputs a wave (131 rows of 28 adapters in turn, 104 x
+// 7680, rank 32 29 -> 20 us; 256 of 24, 4096 x 4096, rank 16 17 -> 14); at higher ranks that takes too many registers (64 rows of 24, rank 128 18 -> 25).
+enum { kWhole, kPast, kParts, kFew, kFewParts };
 
 template <bool F32, int RC, int HOW>
 __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
@@ -468,9 +470,11 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
   const int2 place = place_of<ROWS>(g, m0, lane);
   const int mine = place.y, lane_n = 4 * r16;
 
-  // the rows whose bits are set in `mask`: of adapter ad (-1: none), or of none
-  auto body = [&](int ad, unsigned long long mask) __attribute__((always_inline)) {
-    const int list = nth_of(mask, lane), count = __builtin_popcountll(mask), first = wave * 16;
+  // The rows whose bits are set in `mask`: of adapter ad (-1: none), or of none. FEW: 16 at most; the waves then take blocks of outputs
+  // in turns, with B's values straight from memory.
+  auto body = [&](auto few, int ad, unsigned long long mask) __attribute__((always_inline)) {
+    constexpr bool FEW = decltype(few)::value;
+    const int list = nth_of(mask, lane), count = __builtin_popcountll(mask), first = FEW ? 0 : wave * 16;
     const bool busy = first < count;
     const uint16_t* up = a.b + max(ad, 0) * a.bs;
     int m[4];                                       // rows of the results (behind the last: the first, not stored)
@@ -503,8 +507,22 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
       for (int i = 0; i < 4; ++i) base[i].load(a, m[i], nb * 64 + lane_n);
     };
     // everything that is read goes under way before anything is waited for, the rank among it
-    if (ad >= 0) load_b(nb0);
-    if (busy) load_base(nb0);
+    uint4 bv[FEW ? RC : 1][4];
+    auto load_own = [&](int nb) __attribute__((always_inline)) {
+#pragma unroll
+      for (int rc = 0; rc < (FEW ? RC : 0); ++rc)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          bv[rc][e] = load16(up + (int64_t)min(nb * 64 + 4 * r16 + e, a.N - 1) * a.R + min(rc * 32 + 8 * q4, a.R - 8));
+    };
+    if constexpr (FEW) {
+      if (nb0 + wave >= nb1) return;
+      if (ad >= 0) load_own(nb0 + wave);
+      load_base(nb0 + wave);
+    } else {
+      if (ad >= 0) load_b(nb0);
+      if (busy) load_base(nb0);
+    }
     const int at = __shfl(list, first + r16 < count ? first + r16 : 0, 64), row = __shfl(place.x, at, 64);
     const bool has = __shfl(mine, at, 64) >= 0;
     f32x4 tv[RC][2];
@@ -520,7 +538,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
     if (rank && busy) {
       // the parts in their order, a few asked for at once (one behind the other, 64 rows of 24 adapters, 4096 x 4096, rank 16 / 128 took
       // 11.7 / 24.8 us, so 10.7 / 18.0)
-      if constexpr (HOW == kParts) {
+      if constexpr (HOW == kParts || HOW == kFewParts) {
         auto add = [&](auto count, int z0) __attribute__((always_inline)) {
           constexpr int Z = decltype(count)::value;
           f32x4 more[Z][RC][2];
@@ -561,6 +579,41 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
         }
       }
     }
+    // results of a block, of four rows
+    auto finish = [&](int nb, int next, const f32x4 (&acc)[4]) __attribute__((always_inline)) {
+      // lane holds its outputs of rows 4 q4 + i
+      f32x4 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = base[i].values();
+        if (with[i]) v[i] += f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
+      }
+      if (next < nb1) load_base(next);
+      activate(v, a.act);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (first + 4 * q4 + i < count) store<F32, STREAM>(a, m[i], nb * 64 + lane_n, v[i]);
+    };
+    if constexpr (FEW) {
+      for (int nb = nb0 + wave; nb < nb1; nb += W) {
+        f32x4 acc[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] = f32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int rc = 0; rc < RC; ++rc)
+          if (rc * 32 < rank) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bf16x8 bf = as_bf16x8(first_of(bv[rc][e], rank - rc * 32 - 8 * q4));
+#pragma unroll
+              for (int p = 0; p < PARTS; ++p) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(tf[rc][p]), bf, acc[e], 0, 0, 0);
+            }
+          }
+        if (rank && nb + W < nb1) load_own(nb + W);
+        finish(nb, nb + W, acc);
+      }
+      return;
+    }
     __syncthreads();                                // (the last adapter's block has been read)
     if (rank) keep_b(lds[0], rank);
     __syncthreads();
@@ -581,18 +634,7 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
               for (int p = 0; p < PARTS; ++p) acc[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(tf[rc][p]), bf, acc[e], 0, 0, 0);
             }
           }
-        // lane holds its outputs of rows 4 q4 + i
-        f32x4 v[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          v[i] = base[i].values();
-          if (with[i]) v[i] += f32x4{acc[0][i], acc[1][i], acc[2][i], acc[3][i]};
-        }
-        if (nb + 1 < nb1) load_base(nb + 1);
-        activate(v, a.act);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (first + 4 * q4 + i < count) store<F32, STREAM>(a, m[i], nb * 64 + lane_n, v[i]);
+        finish(nb, nb + 1, acc);
       }
       if (rank && nb + 1 < nb1) {
         keep_b(lds[(nb + 1 - nb0) & 1], rank);
@@ -608,8 +650,16 @@ __global__ __launch_bounds__(256) void k_lora_up(LoraArgs g) {
     const int ad = left ? __builtin_amdgcn_readlane(mine, (int)__builtin_ctzll(left)) : -1;
     const unsigned long long mask = __ballot(mine == ad) & left;
     left &= ~mask;
-    if (j % g.slots == slot) body(ad, j ? mask : mask | none);
-    ++j;
+    if (j++ % g.slots == slot) {
+      const unsigned long long rows = j > 1 ? mask : mask | none;
+      if constexpr (HOW == kFew || HOW == kFewParts) {
+        if (__builtin_popcountll(rows) <= 16) {
+          body(std::true_type(), ad, rows);
+          continue;
+        }
+      }
+      body(std::false_type(), ad, rows);
+    }
   } while (left);
 }
 
@@ -717,11 +767,14 @@ __global__ __launch_bounds__(64 * kWaves) void k_lora(LoraArgs g) {
     if (m0 + 4 * q4 + i < a.M) store<F32, false>(a, m0 + 4 * q4 + i, n0 + 4 * r16, v[i]);
 }
 
-template <bool F32, int HOW>
-hipError_t up(LoraArgs g, hipStream_t s) {
+unsigned up_grid(const LoraArgs& g) {
   const int tiles = (g.a.M + 63) / 64;
-  g.xcds = tiles < 8 ? 1 : 8;
-  const unsigned wgs = (unsigned)((tiles + g.xcds - 1) / g.xcds * g.xcds) * g.slots * g.tiles_n;
+  return (unsigned)((tiles + g.xcds - 1) / g.xcds * g.xcds) * g.slots * g.tiles_n;
+}
+
+template <bool F32, int HOW>
+hipError_t up(const LoraArgs& g, hipStream_t s) {
+  const unsigned wgs = up_grid(g);
   const int rc = (g.a.R + 31) / 32;
   return launch(rc == 1 ? k_lora_up<F32, 1, HOW> : rc == 2 ? k_lora_up<F32, 2, HOW> : k_lora_up<F32, 4, HOW>, dim3(wgs), dim3(256), 0, s, g);
 }
@@ -761,11 +814,17 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   if (p.order) g.order = order;
   g.slots = p.up_slots;
   g.run = p.run;
+  g.xcds = a.M <= 7 * 64 ? 1 : 8;                   // fewer than eight tiles: one
   g.tiles_n = (int)((((int64_t)a.N + 63) / 64 + g.run - 1) / g.run);
   // A result of 16 MiB or more goes past the caches, as its base comes, where rows are whole lines of 128 bytes (8192 rows of 4096 x
   // 4096, rank 64: 69 us instead of 78; 8191 rows of 4096 x 4099, whose lines are written in two parts, 104 so and 85 through the caches).
   const int64_t item = a.f32 ? 4 : 2;
   const bool lines = (((uintptr_t)a.y | (uintptr_t)a.base | (uintptr_t)(a.ldy * item) | (uintptr_t)(a.ldbase * item)) & 127) == 0;
+  if (a.R <= 32 && !p.order && (a.adapters >= 4 || a.M <= 16)) {        // a tile's 64 rows are of so many, or it has no more
+    const auto few = g.splits == 1 ? (a.f32 ? k_lora_up<true, 1, kFew> : k_lora_up<false, 1, kFew>)
+                                   : (a.f32 ? k_lora_up<true, 1, kFewParts> : k_lora_up<false, 1, kFewParts>);
+    return launch(few, dim3(up_grid(g)), dim3(256), 0, s, g);
+  }
   if (g.splits > 1) return a.f32 ? up<true, kParts>(g, s) : up<false, kParts>(g, s);
   if (lines && (int64_t)a.M * a.N * item >= 16 << 20) return a.f32 ? up<true, kPast>(g, s) : up<false, kPast>(g, s);
   return a.f32 ? up<true, kWhole>(g, s) : up<false, kWhole>(g, s);

@@ -53,6 +53,9 @@ LORA = [
     ((8, 4, 1, False, 2), 8191, 520, 70, 72, 5, mixed),
     ((1, 1, 1, False, 2), 16384, 1024, 64, 8, 7, mixed),             # the most rows beside the first product
     ((4, 2, 1, True, 2), 16383, 1032, 70, 40, 2, grouped),
+    ((1, 1, 1, False, 0), 70, 104, 700, 16, 9, mixed),              # adapters of few rows, and of many
+    ((2, 1, 1, False, 0), 200, 72, 333, 32, 4, lambda m, slots: [0] * 100 + [1, 2, 3, -1] * 25),
+    ((2, 1, 2, False, 0), 40, 1032, 500, 24, 6, grouped),
     ((1, 1, 8, False, 0), 2, 4104, 64, 8, 2, mixed),
 ]
 
