@@ -74,8 +74,8 @@ TP_API tp_status tps_cache_read(const tps_cache_rows_args* a, void* stream);
  * query that sees no key, or whose scores are all -infinity, gives zeros. Keys that a query does not see do not touch it, whatever
  * their places hold. Rows i >= q_lens[b] of out are left as they are. kv_len is at least every sequence's length
  * (longer ones are cut to it; max_pages page_size is always enough, and a closer bound plans the call better).
- * Scores, exponentials and sums are fp32. Each exponential (times the scale of its 8-bit v_j) is rounded to bf16
- * before it multiplies v_j, not in the sum that divides; the result is rounded once more: off by 2^-8 of sum softmax_j |v_j| and 2^-8 of itself at
+ * Scores, exponentials and sums are fp32. Each exponential (times the scale of its 8-bit v_j) multiplies v_j as two bf16 parts, which leave
+ * 2^-15 of it; the result is rounded once: off by 2^-15 of sum softmax_j |v_j| and 2^-8 of itself at
  * most. Values of which 2^8 times a query's sum reaches 2^128 may overflow. An infinity or NaN in a seen v_j makes its
  * column infinite or NaN.
  * q and out: bf16, `heads` heads (each key/value head serves heads / kv_heads consecutive ones), strides in elements between
