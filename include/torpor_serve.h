@@ -27,8 +27,8 @@ extern "C" {
  * Values of page p, token t of it, key/value head h start at element p stride[0] + t stride[1] + h stride[2] and are contiguous
  * (head_dim 64 or 128), at 16-byte boundaries: strides in whole 16 bytes, that between tokens at least head_dim and at most
  * 2^23, (page_size - 1) times it below 2^30. TP_BF16: the values. TPS_E4M3: 8-bit floats (4 exponent, 3 mantissa bits, largest 448, no infinities) of which
- * each token's head has a scale 2^(x - 127), x = exps[p][0 for k, 1 for v][h][t] (contiguous, 4-byte aligned, pages 2 kv_heads
- * page_size below 2^31): the smallest power of two, 2^-126 or more, for which no value's magnitude divided by it is
+ * each token's head has a scale 2^(x - 127), NaN if x is 255, x = exps[p][0 for k, 1 for v][h][t] (contiguous, 4-byte aligned, pages 2 kv_heads
+ * page_size below 2^31). tps_cache_append takes the smallest power of two, 2^-126 or more, for which no value's magnitude divided by it is
  * over 448; values divided by it are rounded to the nearest, ties to even (off by at most 2^-4 of themselves, or 2^-10 of the
  * scale). An infinity or NaN becomes NaN, and the scale is that of the others.
  *
@@ -76,7 +76,8 @@ TP_API tp_status tps_cache_read(const tps_cache_rows_args* a, void* stream);
  * (longer ones are cut to it; max_pages page_size is always enough, and a closer bound plans the call better).
  * Scores, exponentials and sums are fp32. Each exponential (times the scale of its 8-bit v_j) multiplies v_j as two bf16 parts, which leave
  * 2^-15 of it; the result is rounded once: off by 2^-15 of sum softmax_j |v_j| and 2^-8 of itself at
- * most. Values of which 2^8 times a query's sum reaches 2^128 may overflow. An infinity or NaN in a seen v_j makes its
+ * most. Values of which 2^8 times a query's sum reaches 2^128 may overflow, and so may the results of a query that sees a v_j
+ * of scale 2^120 or more; what is below 2^-126 may be lost. An infinity or NaN in a seen v_j makes its
  * column infinite or NaN.
  * q and out: bf16, `heads` heads (each key/value head serves heads / kv_heads consecutive ones), strides in elements between
  * sequences, tokens and heads, as in tpo_attention (out's not 0; it overlaps no input). Made for single tokens and a few drafted ones: keys are

@@ -58,12 +58,11 @@ __device__ __forceinline__ uint2 to_e4m3(uint4 w, int* byte) {
   return make_uint2(c[0], c[1]);
 }
 
+// Eight codes times 2^(byte - 127). The conversion takes its scale as an exponent byte, at an fp32 number's place of it: 0 is 2^-127
+// there and 255 NaN (as a number to multiply by they are 0 and infinity), and its one rounding is to the nearest, ties to even.
 __device__ __forceinline__ uint4 from_e4m3(uint2 c, uint32_t byte) {
   const float s = __uint_as_float(byte << 23);
-  auto two = [&](uint32_t x, auto high) {
-    const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.f, decltype(high)::value));
-    return f2bf2(__uint_as_float(b << 16) * s, __uint_as_float(b & 0xffff0000u) * s);
-  };
+  auto two = [&](uint32_t x, auto high) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, s, decltype(high)::value)); };
   return make_uint4(two(c.x, std::false_type()), two(c.x, std::true_type()), two(c.y, std::false_type()), two(c.y, std::true_type()));
 }
 

@@ -18,7 +18,8 @@
 // bf16 parts (rest_of), so that 2^-15 of each is lost: with one, the error against 64 bits was 0.0021 to 0.0023 (norm over norm), where the
 // result's rounding alone gives 0.0017; the second takes 1 to 3% of a call (24 tokens over up to 4096 66.1 -> 66.7 us). 8-bit keys
 // become bf16 exactly, times their scale, as they are read (v_cvt_scalef32_pk_bf16_fp8); 8-bit values become bf16
-// without it, and their scale multiplies the exponential before that is taken apart. The sum that divides is of the exponentials as they are.
+// without it, and their scale multiplies the exponential before that is taken apart (scale byte 255, NaN to the conversion, is an infinite
+// factor there, whose rest is NaN). The sum that divides is of the exponentials as they are.
 // The reference that exponents are taken from follows the maximum only when that has risen by 8 (a factor of 256, harmless in
 // fp32 sums and in bf16, whose precision is relative).
 //
@@ -276,7 +277,7 @@ __global__ __launch_bounds__(64 * W) void k_cache_attention(CacheAttnArgs g) {
       for (int hb = 0; hb < 2; ++hb) {
         const uint32_t x = *reinterpret_cast<const uint32_t*>(base + 2 * T::KB + 32 + 16 * hb + 4 * q4);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) vs[hb][i] = __uint_as_float((x >> (8 * i) & 255u) << 23);
+        for (int i = 0; i < 4; ++i) vs[hb][i] = __uint_as_float(max((x >> (8 * i) & 255u) << 23, 0x400000u));         // byte 0: 2^-127
       }
     }
     uint4 pb[RB], pr[RB];                           // first parts, rests
