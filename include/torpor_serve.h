@@ -6,7 +6,8 @@
  * Conventions, scratch and streams as in torpor_ops.h: TP_OK or a negative TP_E_* code with a message in tp_last_error(); invalid
  * arguments launch nothing; calls are asynchronous on `stream`, allocate nothing, keep nothing from one call for the next,
  * may be captured into a graph and may come from several host threads; `work` (256-byte aligned, may be NULL) needs no preparation,
- * is undefined afterwards, and calls that may overlap need scratch of their own. TPO_WORK_BYTES is as much as any call uses.
+ * is undefined afterwards, and calls that may overlap need scratch of their own. A call uses what fits; TPO_WORK_BYTES is what the calls are
+ * made for. (More lets attention split many rows' long caches further, and adapters take more than 64,000 rows at once.)
  */
 #ifndef TORPOR_SERVE_H
 #define TORPOR_SERVE_H
@@ -113,7 +114,8 @@ TP_API tp_status tps_cache_attention(const tps_cache_attention_args* a, void* st
  * Products are exact, sums fp32; the inner sums times the scale are rounded to two bf16 parts (2^-16 of themselves) for the second product; one
  * rounding of the result. A row's result depends on its own values and adapter alone, whatever others
  * hold; an infinity or NaN among these makes results infinite or NaN. Inner sums beyond bf16's range overflow. M = 0 does nothing. M in whole 16s times N in whole 256s is below 2^36.
- * work holds the inner sums; less of it than 4 M R bytes, or none, computes them anew for every block of outputs. */
+ * work holds the inner sums; with less of it than 4 M (R + 2) bytes rows are taken part after part, and with less than 1024 of them need (4096 where
+ * N is 256 or less), or none, the inner sums are computed anew for every 256 outputs. */
 typedef struct {
   const void* x;
   int64_t ldx;

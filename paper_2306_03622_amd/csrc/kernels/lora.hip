@@ -7,7 +7,8 @@
 // sorting, and no row meets another's adapter. Where there are few tiles, the adapters of a tile go to several workgroups.
 // Where many tiles could hold many adapters each, k_lora_order first writes down the rows adapter by adapter, and tiles are of that order;
 // where a tile holds few, one more workgroup of k_lora_down does so for k_lora_up.
-// Without scratch k_lora does both in one launch and computes t anew for every 256 outputs.
+// Without scratch k_lora does both in one launch and computes t anew for every 256 outputs; where scratch holds t of a part of the rows, they are
+// taken part by part (lora_rows).
 //
 // t is taken as bf16 parts (two, three for fp32 results: 2^-16 and 2^-24 of t), all multiplied by B, whose values are bf16 as they are.
 // Operands: A's rows r against x's rows m (t^T), then t's rows m against B's rows n, those of four blocks interleaved so
@@ -779,17 +780,12 @@ hipError_t up(const LoraArgs& g, hipStream_t s) {
   return launch(rc == 1 ? k_lora_up<F32, 1, HOW> : rc == 2 ? k_lora_up<F32, 2, HOW> : k_lora_up<F32, 4, HOW>, dim3(wgs), dim3(256), 0, s, g);
 }
 
-}  // namespace
-
-hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
-  if (!a.x || !a.a || !a.b || !a.adapter || !a.y || a.M < 1 || a.N < 1 || a.K < 8 || a.K % 8 || a.R < 8 || a.R % 8 || a.R > kLoraRank ||
-      a.adapters < 1)
-    return hipErrorInvalidValue;
+// All rows of a call, or a part of them.
+hipError_t rows_of(const Lora& a, const Split& sp, hipStream_t s) {
   LoraArgs g{};
   g.a = a;
   g.t = sp.partials;
   g.tiles_n = (int)(((int64_t)a.N + 255) / 256);
-  if (((int64_t)a.M + 15) / 16 * g.tiles_n >= 1 << 24) return hipErrorInvalidValue;
   const LoraPlan p = lora_plan(a.M, a.N, a.K, a.R, a.adapters, sp.partials ? sp.partial_bytes : 0);
   if (p.splits == 0)
     return launch(a.f32 ? k_lora<true> : k_lora<false>, dim3((unsigned)((a.M + 15) / 16 * g.tiles_n)), dim3(64 * kWaves), 0, s, g);
@@ -828,6 +824,27 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
   if (g.splits > 1) return a.f32 ? up<true, kParts>(g, s) : up<false, kParts>(g, s);
   if (lines && (int64_t)a.M * a.N * item >= 16 << 20) return a.f32 ? up<true, kPast>(g, s) : up<false, kPast>(g, s);
   return a.f32 ? up<true, kWhole>(g, s) : up<false, kWhole>(g, s);
+}
+
+}  // namespace
+
+hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
+  if (!a.x || !a.a || !a.b || !a.adapter || !a.y || a.M < 1 || a.N < 1 || a.K < 8 || a.K % 8 || a.R < 8 || a.R % 8 || a.R > kLoraRank ||
+      a.adapters < 1)
+    return hipErrorInvalidValue;
+  if (((int64_t)a.M + 15) / 16 * (((int64_t)a.N + 255) / 256) >= 1 << 24) return hipErrorInvalidValue;
+  const int64_t rows = lora_rows(a.M, a.N, a.K, a.R, a.adapters, sp.partials ? sp.partial_bytes : 0), item = a.f32 ? 4 : 2;
+  for (int64_t m0 = 0; m0 < a.M; m0 += rows) {
+    Lora part = a;
+    part.M = (int)std::min<int64_t>(rows, a.M - m0);
+    part.x += m0 * a.ldx;
+    part.adapter += m0;
+    if (a.base) part.base = static_cast<const char*>(a.base) + m0 * a.ldbase * item;
+    part.y = static_cast<char*>(a.y) + m0 * a.ldy * item;
+    const hipError_t e = rows_of(part, sp, s);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace k

@@ -46,5 +46,20 @@ inline LoraPlan lora_plan(int64_t M, int64_t N, int64_t K, int64_t R, int64_t ad
   return {(int)z, tall, (int)ds, (int)us, (int)run, order};
 }
 
+// Rows that are taken at once: all of them where scratch holds their inner sums (and their order, where they are put in one), else
+// parts one after the other, each with launches of its own: multiples of 64 rows, as few and as even as the scratch allows. Parts have 1024 rows at
+// least, and 4096 where one launch computes the inner sums once; below, everything goes in one launch. us, graph replay, one launch / parts of
+// 512 / 1024 / 4096 rows: 4096 rows of 4096 x 4096, 32 adapters of rank 16 2028 / 140 / 77 / 32, 16384 of 2048 x 2048, four of 32 806 / 318 / 210 / 95, 4096 of
+// 256 -> 4096, one of 16 34 / 73 / 44 / 22, 1024 -> 1024, one of 64 38 / 91 / 46 / 20; to 256 outputs: 4096 of 4096, one of 64
+// 55 / 117 / 61 / 23, 16384 of 1024, four of 64 133 / 347 / 176 / 68.
+inline int64_t lora_rows(int64_t M, int64_t N, int64_t K, int64_t R, int64_t adapters, uint64_t scratch) {
+  const int64_t words = (int64_t)(scratch / 4), least = N <= 256 ? 4096 : 1024;
+  const int64_t most = std::min<int64_t>(words / (R + 2), (1 << 27) - 1) / 64 * 64;        // (a call in two launches has fewer than 2^27 rows)
+  if (most < least || (M <= words / (R + 2) && M < 1 << 27)) return M;
+  if (M <= words / R && M < 1 << 27 && lora_plan(M, N, K, R, adapters, ~0ull >> 1).order == 0) return M;
+  const int64_t parts = (M + most - 1) / most, rows = (M + parts - 1) / parts;
+  return std::max(least, (rows + 63) / 64 * 64);
+}
+
 }  // namespace k
 }  // namespace tp
