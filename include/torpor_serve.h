@@ -111,9 +111,10 @@ TP_API tp_status tps_cache_attention(const tps_cache_attention_args* a, void* st
  * contiguous; R a multiple of 8 up to 128, K of 8 up to 2^20. x, A and B start at 16-byte boundaries, a_stride
  * and b_stride are multiples of 8. ranks (device, NULL: R for all) are clamped to [0, R]: what lies behind an adapter's rank is not
  * used, whatever it holds. scales (device, fp32, NULL: 1).
- * Products are exact, sums fp32; the inner sums times the scale are rounded to two bf16 parts (2^-16 of themselves) for the second product; one
- * rounding of the result. A row's result depends on its own values and adapter alone, whatever others
- * hold; an infinity or NaN among these makes results infinite or NaN. Inner sums beyond bf16's range overflow. M = 0 does nothing. M in whole 16s times N in whole 256s is below 2^36.
+ * Products are exact, sums fp32; the inner sums times the scale are rounded to two bf16 parts (2^-16 of themselves; three, 2^-24, for fp32 results)
+ * for the second product; one rounding of the result. A row's result depends on its own values and adapter alone, whatever others
+ * hold and wherever in the call it stands (M, N and work_bytes choose the order of addition, so that between calls that differ in these its
+ * last bits may differ); an infinity or NaN among these makes results infinite or NaN. Inner sums beyond bf16's range overflow. M = 0 does nothing. M in whole 16s times N in whole 256s is below 2^36.
  * work holds the inner sums; with less of it than 4 M (R + 2) bytes rows are taken part after part, and with less than 1024 of them need (4096 where
  * N is 256 or less), or none, the inner sums are computed anew for every 256 outputs. */
 typedef struct {
