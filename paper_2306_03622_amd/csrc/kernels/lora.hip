@@ -780,13 +780,12 @@ hipError_t up(const LoraArgs& g, hipStream_t s) {
   return launch(rc == 1 ? k_lora_up<F32, 1, HOW> : rc == 2 ? k_lora_up<F32, 2, HOW> : k_lora_up<F32, 4, HOW>, dim3(wgs), dim3(256), 0, s, g);
 }
 
-// All rows of a call, or a part of them.
-hipError_t rows_of(const Lora& a, const Split& sp, hipStream_t s) {
+// All rows of a call, or a part of them. p: the plan of a whole part, for the last one too, so that every row's sums are added in the same order.
+hipError_t rows_of(const Lora& a, const LoraPlan& p, const Split& sp, hipStream_t s) {
   LoraArgs g{};
   g.a = a;
   g.t = sp.partials;
   g.tiles_n = (int)(((int64_t)a.N + 255) / 256);
-  const LoraPlan p = lora_plan(a.M, a.N, a.K, a.R, a.adapters, sp.partials ? sp.partial_bytes : 0);
   if (p.splits == 0)
     return launch(a.f32 ? k_lora<true> : k_lora<false>, dim3((unsigned)((a.M + 15) / 16 * g.tiles_n)), dim3(64 * kWaves), 0, s, g);
   g.splits = p.splits;
@@ -833,7 +832,9 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
       a.adapters < 1)
     return hipErrorInvalidValue;
   if (((int64_t)a.M + 15) / 16 * (((int64_t)a.N + 255) / 256) >= 1 << 24) return hipErrorInvalidValue;
-  const int64_t rows = lora_rows(a.M, a.N, a.K, a.R, a.adapters, sp.partials ? sp.partial_bytes : 0), item = a.f32 ? 4 : 2;
+  const uint64_t scratch = sp.partials ? sp.partial_bytes : 0;
+  const int64_t rows = lora_rows(a.M, a.N, a.K, a.R, a.adapters, scratch), item = a.f32 ? 4 : 2;
+  const LoraPlan plan = lora_plan(rows, a.N, a.K, a.R, a.adapters, scratch);
   for (int64_t m0 = 0; m0 < a.M; m0 += rows) {
     Lora part = a;
     part.M = (int)std::min<int64_t>(rows, a.M - m0);
@@ -841,7 +842,7 @@ hipError_t lora(const Lora& a, const Split& sp, hipStream_t s) {
     part.adapter += m0;
     if (a.base) part.base = static_cast<const char*>(a.base) + m0 * a.ldbase * item;
     part.y = static_cast<char*>(a.y) + m0 * a.ldy * item;
-    const hipError_t e = rows_of(part, sp, s);
+    const hipError_t e = rows_of(part, plan, sp, s);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;

@@ -50,3 +50,15 @@ def test_parts(m, k, n, r, slots, ids, rows, f32):
     got = s.run("relu", work=work, base=row)
     s.base = row.contiguous()
     s.check(got, "relu")
+
+
+def test_a_row_gives_the_same_bits_in_every_part():
+    # (the last part has two rows of long sums: by itself its plan would split them, and add in another order)
+    import torch
+    m, k, n, r, slots = 2050, 2064, 300, 16, 3
+    s = Setup(1300, m, k, n, r, slots, True, mixed(m, slots))
+    _, work = guarded(4 * 1024 * (r + 2))
+    x, adapter, base, want = s.x, s.adapter, s.base, s.run(work=work)
+    for p in (torch.arange(m - 1, -1, -1, device="cuda:0"), torch.roll(torch.arange(m, device="cuda:0"), 700)):
+        s.x, s.adapter, s.base = x[p].contiguous(), adapter[p].contiguous(), base[p].contiguous()
+        assert torch.equal(s.run(work=work), want[p])
