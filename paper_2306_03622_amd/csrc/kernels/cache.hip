@@ -8,6 +8,7 @@
 // 8-bit rows: a = max |x| over the finite values of the head, s = 2^e the smallest power of two
 // with a <= 448 s = 1.75 2^8 s: for a = m 2^x, 1 <= m < 2, e = x - 8, or x - 7 where m > 1.75. Division by s is exact (a power of two), so
 // the one rounding is the conversion's. Reading back, code * s has four significant bits: exact in bf16 unless it leaves its range.
+#include "cache_plan.hpp"
 #include "serve_args.hpp"
 
 namespace tp {
@@ -15,8 +16,7 @@ namespace k {
 
 struct CacheRowsArgs {
   CacheRows a;
-  int per, cols;          // lanes that a token takes, workgroups side by side for one (more than 1: then a row at a time)
-  int rows, blocks;       // rows side by side in a workgroup, workgroups along the rows
+  int per, cols, rows, blocks;      // CacheRowsPlan
 };
 
 template <>
@@ -147,19 +147,14 @@ hipError_t rows(const CacheRows& a, hipStream_t s) {
   if (!a.c.k || !a.c.v || (a.c.e4m3 && !a.c.exps) || !a.p.table || !a.p.kv_lens || !a.k || !a.v || (a.c.dim != 64 && a.c.dim != 128) ||
       a.p.batch < 1 || a.p.q_len < 1 || a.c.heads < 1 || a.c.heads > 65536 || a.c.pages < 1 || a.p.max_pages < 1 || a.c.lg < 4 || a.c.lg > 12)
     return hipErrorInvalidValue;
+  const CacheRowsPlan p = cache_rows_plan(a.c.dim, a.c.heads, a.p.batch, a.p.q_len);
+  const int64_t wgs = p.blocks * p.cols * a.p.batch;
+  if (wgs >= 1 << 24) return hipErrorInvalidValue;
   CacheRowsArgs g{};
   g.a = a;
-  g.per = a.c.heads * (a.c.dim / 8);
-  g.cols = (g.per + 255) / 256;
-  g.rows = g.cols > 1 ? 1 : 256 / g.per;
-  // two rows in each place where that still gives every CU two workgroups (two prompts of 3001 in 8 bits 8.8 us, with four 9.8, one 9.4)
-  auto blocks = [&](int u) { return ((int64_t)a.p.q_len + (int64_t)g.rows * u - 1) / ((int64_t)g.rows * u); };
-  const int u = blocks(2) * g.cols * a.p.batch >= 512 ? 2 : 1;
-  const int64_t wgs = blocks(u) * g.cols * a.p.batch;
-  if (wgs >= 1 << 24) return hipErrorInvalidValue;
-  g.blocks = (int)blocks(u);
-  if (a.c.e4m3) return a.c.dim == 64 ? go<64, true, APPEND>(g, wgs, u, s) : go<128, true, APPEND>(g, wgs, u, s);
-  return a.c.dim == 64 ? go<64, false, APPEND>(g, wgs, u, s) : go<128, false, APPEND>(g, wgs, u, s);
+  g.per = p.per, g.cols = p.cols, g.rows = p.rows, g.blocks = (int)p.blocks;
+  if (a.c.e4m3) return a.c.dim == 64 ? go<64, true, APPEND>(g, wgs, p.each, s) : go<128, true, APPEND>(g, wgs, p.each, s);
+  return a.c.dim == 64 ? go<64, false, APPEND>(g, wgs, p.each, s) : go<128, false, APPEND>(g, wgs, p.each, s);
 }
 
 }  // namespace

@@ -1,10 +1,29 @@
-// How a call of the attention over a paged cache is split (no HIP headers: also compiled for the host alone).
+// How calls on a paged cache, rows in and out of it and attention over it, are split (no HIP headers: also compiled for the host alone).
 #pragma once
 #include <algorithm>
 #include <cstdint>
 
 namespace tp {
 namespace k {
+
+struct CacheRowsPlan {
+  int per, cols;          // lanes that a token takes, workgroups of 256 side by side for one (more than 1: then a row at a time)
+  int rows, each;         // rows side by side in a workgroup, rows in each place
+  int64_t blocks;         // workgroups along a sequence's rows
+};
+
+// heads: key/value heads; q_len: rows of each of `batch` sequences.
+inline CacheRowsPlan cache_rows_plan(int dim, int64_t heads, int64_t batch, int64_t q_len) {
+  CacheRowsPlan p{};
+  p.per = (int)heads * (dim / 8);
+  p.cols = (p.per + 255) / 256;
+  p.rows = p.cols > 1 ? 1 : 256 / p.per;
+  // two rows in each place where that still gives every CU two workgroups (two prompts of 3001 in 8 bits 8.8 us, with four 9.8, one 9.4)
+  auto blocks = [&](int64_t each) { return (q_len + p.rows * each - 1) / (p.rows * each); };
+  p.each = blocks(2) * p.cols * batch >= 512 ? 2 : 1;
+  p.blocks = blocks(p.each);
+  return p;
+}
 
 struct CachePlan {
   int rb, waves, splits;  // blocks of 16 rows a workgroup takes, its waves over the keys, workgroups over the keys
