@@ -19,11 +19,6 @@ struct CacheRowsArgs {
   int per, cols, rows, blocks;      // CacheRowsPlan
 };
 
-template <>
-struct PtrFields<CacheRowsArgs> {
-  static void add(std::vector<uint32_t>& v, uint32_t at) { PtrFields<CacheRows>::add(v, at + (uint32_t)offsetof(CacheRowsArgs, a)); }
-};
-
 namespace {
 
 template <int CTRL>

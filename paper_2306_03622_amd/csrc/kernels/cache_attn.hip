@@ -40,16 +40,6 @@ struct CacheAttnArgs {
   float* part;            // splits > 1: [split][slot][dim] sums, then [split][slot][2] maximum and sum
 };
 
-template <>
-struct PtrFields<CacheAttnArgs> {
-  static void add(std::vector<uint32_t>& v, uint32_t at) {
-    constexpr size_t a = offsetof(CacheAttnArgs, a), c = a + offsetof(CacheAttention, c), p = a + offsetof(CacheAttention, p);
-    add_ptrs(v, at, {c + offsetof(Cache, k), c + offsetof(Cache, v), c + offsetof(Cache, exps), p + offsetof(Pages, table),
-                     p + offsetof(Pages, q_lens), p + offsetof(Pages, kv_lens), a + offsetof(CacheAttention, q),
-                     a + offsetof(CacheAttention, out), offsetof(CacheAttnArgs, part)});
-  }
-};
-
 namespace {
 
 typedef short v4s __attribute__((ext_vector_type(4)));

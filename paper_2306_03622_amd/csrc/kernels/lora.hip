@@ -30,16 +30,6 @@ struct LoraArgs {
   int run, xcds;          // second product: blocks of 64 outputs a workgroup, XCDs that tiles are handed to
 };
 
-template <>
-struct PtrFields<LoraArgs> {
-  static void add(std::vector<uint32_t>& v, uint32_t at) {
-    PtrFields<Lora>::add(v, at + (uint32_t)offsetof(LoraArgs, a));
-    v.push_back(at + (uint32_t)offsetof(LoraArgs, t));
-    v.push_back(at + (uint32_t)offsetof(LoraArgs, order));
-    v.push_back(at + (uint32_t)offsetof(LoraArgs, order_out));
-  }
-};
-
 namespace {
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -233,7 +223,7 @@ __global__ __launch_bounds__(1024) void k_lora_order(LoraArgs g) {
 // Workgroups are handed out to the eight XCDs in turn: tiles side by side, whose rows often have the same adapter, for one XCD.
 __device__ __forceinline__ int tile_of(int id, int tiles) {
   const int each = tiles >> 3, more = tiles & 7, x = id & 7;
-  return id >= each * 8 + more ? id : x * each + min(x, more) + (id >> 3);
+  return x * each + min(x, more) + (id >> 3);
 }
 
 // The same order for up to seven adapters and kLoraFewRows rows, by one workgroup of W waves: every lane has a run of rows, whose

@@ -1,31 +1,10 @@
-// What the serving operators' kernels share: the pointers of their argument blocks and a sequence's lengths.
+// What the serving operators' kernels share: a sequence's lengths. (No model's graph runs them, so their argument blocks name no pointers to
+// the launch log, as those of gemm_args.hpp do.)
 #pragma once
 #include "common.hpp"
 
 namespace tp {
 namespace k {
-
-inline void add_ptrs(std::vector<uint32_t>& v, uint32_t at, std::initializer_list<size_t> fields) {
-  for (size_t o : fields) v.push_back(at + (uint32_t)o);
-}
-
-template <>
-struct PtrFields<CacheRows> {
-  static void add(std::vector<uint32_t>& v, uint32_t at) {
-    add_ptrs(v, at, {offsetof(CacheRows, c) + offsetof(Cache, k), offsetof(CacheRows, c) + offsetof(Cache, v),
-                     offsetof(CacheRows, c) + offsetof(Cache, exps), offsetof(CacheRows, p) + offsetof(Pages, table),
-                     offsetof(CacheRows, p) + offsetof(Pages, q_lens), offsetof(CacheRows, p) + offsetof(Pages, kv_lens),
-                     offsetof(CacheRows, k), offsetof(CacheRows, v)});
-  }
-};
-
-template <>
-struct PtrFields<Lora> {
-  static void add(std::vector<uint32_t>& v, uint32_t at) {
-    add_ptrs(v, at, {offsetof(Lora, x), offsetof(Lora, a), offsetof(Lora, b), offsetof(Lora, adapter), offsetof(Lora, ranks),
-                     offsetof(Lora, scales), offsetof(Lora, base), offsetof(Lora, y)});
-  }
-};
 
 // New and held tokens of a sequence.
 struct Lens {
