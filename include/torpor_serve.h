@@ -77,8 +77,8 @@ TP_API tp_status tps_cache_read(const tps_cache_rows_args* a, void* stream);
  * (longer ones are cut to it; max_pages page_size is always enough, and a closer bound plans the call better).
  * Scores, exponentials and sums are fp32. Each exponential (times the scale of its 8-bit v_j) multiplies v_j as two bf16 parts, which leave
  * 2^-15 of it; the result is rounded once: off by 2^-15 of sum softmax_j |v_j| and 2^-8 of itself at
- * most. Values of which 2^8 times a query's sum reaches 2^128 may overflow, and so may the results of a query that sees a v_j
- * of scale 2^120 or more; what is below 2^-126 may be lost. An infinity or NaN in a seen v_j makes its
+ * most. Values of which 2^8 times a query's sum reaches 2^128 may overflow, and so may the results of a query that sees an
+ * 8-bit v_j of scale 2^120 or more; scales below 2^-100 leave fewer bits, nothing of what is below 2^-126. An infinity or NaN in a seen v_j makes its
  * column infinite or NaN.
  * q and out: bf16, `heads` heads (each key/value head serves heads / kv_heads consecutive ones), strides in elements between
  * sequences, tokens and heads, as in tpo_attention (out's not 0; it overlaps no input). Made for single tokens and a few drafted ones: keys are
@@ -105,7 +105,8 @@ TP_API tp_status tps_cache_attention(const tps_cache_attention_args* a, void* st
  *
  * y[m][n] = act(base[m][n] + scale_a sum_{r < rank_a} (sum_k x[m][k] A_a[r][k]) B_a[n][r]), a = adapter[m], m < M, n < N.
  * A row whose adapter is not in [0, adapters) has none: y = act(base). Rows may name adapters in any order; adapters that no
- * row names are not read.
+ * row names are not read. Rows of many adapters in turn are put in order for pools of fewer than 4096 adapters and up to 2^17 rows at once; beyond, the
+ * adapters of 64 rows are taken one after the other, and slowly.
  * x bf16, rows ldx apart (a multiple of 8); y and base bf16 or fp32 (dtype), rows ldy and ldbase apart, base NULL: zeros. y may be base (same row
  * stride), else it overlaps no input. A [adapters][R][K] and B [adapters][N][R] bf16, adapters a_stride and b_stride elements apart, rows
  * contiguous; R a multiple of 8 up to 128, K of 8 up to 2^20. x, A and B start at 16-byte boundaries, a_stride

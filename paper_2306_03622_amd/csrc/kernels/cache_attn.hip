@@ -16,7 +16,8 @@
 // exponentials, in bf16 as the matrix cores take V, are then the next product's operand where they are, if its
 // 32 keys are taken in that order: O^T = V^T P^T, with V^T read by the transposing LDS loads in the same order of keys. They go in as two
 // bf16 parts (rest_of), so that 2^-15 of each is lost: with one, the error against 64 bits was 0.0021 to 0.0023 (norm over norm), where the
-// result's rounding alone gives 0.0017; the second takes 1 to 3% of a call (24 tokens over up to 4096 66.1 -> 66.7 us). 8-bit keys
+// result's rounding alone gives 0.0017; the second takes 1 to 4% of a call (24 tokens over up to 4096 66.1 -> 66.8 us, 64 over up to 500 22.8 -> 23.4, 8 new tokens of two sequences over up to 20,000 in
+// 8 bits 27.8 -> 29.9). 8-bit keys
 // become bf16 exactly, times their scale, as they are read (v_cvt_scalef32_pk_bf16_fp8); 8-bit values become bf16
 // without it, and their scale multiplies the exponential before that is taken apart (scale byte 255, NaN to the conversion, is an infinite
 // factor there, whose rest is NaN). The sum that divides is of the exponentials as they are.
@@ -547,8 +548,8 @@ hipError_t go(CacheAttnArgs g, hipStream_t s) {
   if (wgs * 64 * W >= 1ll << 32) return hipErrorInvalidValue;
   hipError_t e = launch((k_cache_attention<D, E4M3, RB, W, NST>), dim3((unsigned)wgs), dim3(64 * W), 0, s, g);
   if (e != hipSuccess || g.splits == 1) return e;
-  // A workgroup per row where its splits are more than a wave asks for at once, and rows few (us, a wave / a workgroup: one token of 8 heads
-  // on one, 64 values, over 60,000 21.6 / 15.5; two of 4096 11.0 / 9.4; one of 32 heads over 100,001 in 8 bits 49.7 / 48.7).
+  // A workgroup per row where its splits are more than a wave asks for at once, and rows few (us, a wave / a workgroup, with exponentials in
+  // one part: one token of 8 heads on one, 64 values, over 60,000 21.6 / 15.5, with two 15.9; two of 4096 11.0 / 9.4; one of 32 heads over 100,001 in 8 bits 49.7 / 48.7).
   if (g.splits > 16 && rows * heads <= 4096) return launch((k_cache_join<D, true>), dim3((unsigned)(rows * heads)), dim3(256), 0, s, g);
   return launch((k_cache_join<D, false>), dim3((unsigned)((rows * heads + 3) / 4)), dim3(256), 0, s, g);
 }

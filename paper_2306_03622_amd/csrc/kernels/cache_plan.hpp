@@ -43,7 +43,7 @@ inline CachePlan cache_plan(int dim, bool e4m3, int64_t rows, int64_t heads, int
   if (rb == 1 && span <= 64) return {1, 1, 1};
   const int64_t fits = (int64_t)(scratch / 4) / (rows * heads * (dim + 2));
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>({64, span / 128, fits, ((1 << 24) - 1) / wgs}));       // grids below 2^32 lanes
-  // Time by a model, in ns and bytes: a workgroup takes 3500 beside its keys, which come at 5400 for all, at most 7.5 (8 bits: 5.5) for
+  // (Times here with exponentials in one part; the second adds 1 to 4% to both sides.) Time by a model, in ns and bytes: a workgroup takes 3500 beside its keys, which come at 5400 for all, at most 7.5 (8 bits: 5.5) for
   // a wave; on a CU run as many workgroups as its LDS holds. Where lengths differ they are taken to be three quarters of the longest on
   // average, short ones making room for the next. Partial results are written and read at 5000, and joined in 3000. Of 20 shapes the
   // choice was within 7% of the best of 22. Two waves instead of four (us): 32 / 8 heads of 128, 64 sequences of up to 128 / 256 / 500
