@@ -74,7 +74,7 @@ TP_API tp_status tps_cache_read(const tps_cache_rows_args* a, void* stream);
  * and (j < sinks or window < 0 or j >= p - window), and j is in a page. out = sum over the seen j of softmax_j(scale q k_j) v_j; a
  * query that sees no key, or whose scores are all -infinity, gives zeros. Keys that a query does not see do not touch it, whatever
  * their places hold. Rows i >= q_lens[b] of out are left as they are. kv_len is at least every sequence's length
- * (longer ones are cut to it; max_pages page_size is always enough, and a closer bound plans the call better).
+ * (longer ones are cut to it; below 2^30; max_pages page_size, or 2^30 - 1, is always enough, and a closer bound plans the call better).
  * Scores, exponentials and sums are fp32. Each exponential (times the scale of its 8-bit v_j) multiplies v_j as two bf16 parts, which leave
  * 2^-15 of it; the result is rounded once: off by 2^-15 of sum softmax_j |v_j| and 2^-8 of itself at
  * most. Values of which 2^8 times a query's sum reaches 2^128 may overflow, and so may the results of a query that sees an

@@ -8,6 +8,7 @@ import struct
 from .torpor import TP_ACT, TP_BF16, TP_F32, TP_OK, _P, _check, _stream_of, lib
 
 TPS_E4M3 = 16
+_MOST_TOKENS = (1 << 30) - 1              # of a sequence
 
 
 class tps_cache(C.Structure):
@@ -193,7 +194,7 @@ def tps_cache_read(cache: PagedCache, table, kv_lens, k, v, q_lens=None, stream=
 def tps_cache_attention(cache: PagedCache, table, kv_lens, q, out, q_lens=None, kv_len: int | None = None, window: int = -1, sinks: int = 0,
                         scale: float = 0.0, work=None, stream=None):
     """Attention of the new tokens' q [B][q_len][heads][dim] over the cache, which holds their keys and values already, into out
-    (as q), bf16, in causal order. kv_len: no sequence is longer (default: what the table has room for); window: keys to the
+    (as q), bf16, in causal order. kv_len: no sequence is longer (default: what the table has room for, up to 2^30 - 1); window: keys to the
     left of a token that it sees (negative: all); sinks: first keys that it sees besides; see torpor_serve.h."""
     torch, current, here, _, _, call, _ = _calls or _serve_calls()
     dev, packed, _, dim, size = cache._packed
@@ -212,7 +213,7 @@ def tps_cache_attention(cache: PagedCache, table, kv_lens, q, out, q_lens=None, 
     columns = table.shape[1]
     wp, wb = (0, 0) if work is None else _scratch(work, dev)
     packed += _ATTENTION.pack(table.data_ptr(), table.stride(0), 0 if q_lens is None else q_lens.data_ptr(), kv_lens.data_ptr(), q.data_ptr(),
-                              out.data_ptr(), q0, q1, q2, o0, o1, o2, b, h, n, columns * size if kv_len is None else kv_len, columns, window,
+                              out.data_ptr(), q0, q1, q2, o0, o1, o2, b, h, n, min(columns * size, _MOST_TOKENS) if kv_len is None else kv_len, columns, window,
                               sinks, scale, wp, wb)
     s = current(dev) if stream is None else _stream_of(dev, stream)
     status = call(packed, s) if s or here() == dev else _on_device(torch, call, packed, dev, s)
